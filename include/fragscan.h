@@ -350,6 +350,125 @@ fs_status fs_fragment_table(const fs_net *net, int32_t H, int32_t W, int32_t *h_
 fs_status fs_reassembly_index(const fs_net *net, int32_t H, int32_t W, int32_t *h_out,
                               size_t capacity, size_t *n_needed);
 
+/* ---------------------------------------------------------------------------
+ * Rows: what a program does with a net's answers, and how it fits the last
+ * layer without touching the net.  A row is one window of an output map
+ * (fs_scan's d_out is rows = B * out_h * out_w of n_classes scores when the
+ * last layer has no softmax) or any other vector of scores or features.
+ *
+ * Conventions of the calls below
+ *   - dtype is the storage type of scores, rows, weights, factors and of
+ *     their gradients: FS_F32, or FS_BF16 (every sum, maximum and statistic is
+ *     held in float32 or more, each result rounded once).  Everything named
+ *     float is float32 in both.
+ *   - Strides count elements between the starts of consecutive rows.  An
+ *     input's may be any number >= 0 (0: every row the same), an output's at
+ *     least the row's length.  Elements of a row are adjacent.  Pointers need
+ *     the alignment of their element type only; workspaces 256 bytes.
+ *   - rows may be 0 (nothing is enqueued, but for the zeros of d_ga and d_gb)
+ *     and is below 2^31; sizes and types are checked all the same.
+ *   - Index arrays (labels, adapter numbers) are device memory, read by the
+ *     kernels: a bad value cannot be refused by the call and never reads
+ *     outside the arrays, it gives rows of NaN as stated.
+ *   - Buffers must not overlap unless stated.  Calls are asynchronous on
+ *     `stream`, which must belong to the current device, allocate nothing, and
+ *     may be captured into a HIP graph.  Calls with distinct outputs and
+ *     workspaces may run concurrently.  The results of a call do not depend on
+ *     what runs beside it: the same inputs give the same bits.
+ * ------------------------------------------------------------------------- */
+
+#define FS_MAX_CLASSES (1 << 24) /* classes of a row */
+#define FS_MAX_TOP 64            /* best classes fs_logprobs lists */
+#define FS_MAX_RANK 128          /* rank of an adapter */
+#define FS_MAX_FEATURES (1 << 20) /* inputs or outputs of fs_project */
+
+/* Log probabilities of given labels, entropy and best classes of rows of
+ * scores.  With x a row, T the temperature, m = max x and S = sum_j
+ * exp((x_j - m) / T):
+ *   d_norm[row]    = (m, ln S), two floats; log probability of class j is
+ *                    (x_j - m) / T - ln S
+ *   d_logp[row]    = the log probability of class d_labels[row]; 0 for a
+ *                    negative label (none), NaN for one >= classes
+ *   d_entropy[row] = - sum_j p_j ln p_j
+ *   d_top_id, d_top_logp [rows][n_top] = the n_top classes of largest score,
+ *                    best first, equal scores in the order of their numbers,
+ *                    and their log probabilities
+ * A score of -inf rules its class out (probability 0, never listed: places no
+ * class takes hold -1 and -inf).  A row of nothing but -inf has norm (-inf,
+ * 0), entropy 0, log probability -inf for every label and an empty list.  A
+ * row that holds a NaN or +inf gives NaN throughout and -1 in its list.
+ * Any output may be NULL if another is not; d_logp needs d_labels.
+ * FS_ERR_INVALID_ARG for a temperature that is not above 0 or whose inverse
+ * is not finite, n_top outside 0 .. FS_MAX_TOP, classes outside 1 ..
+ * FS_MAX_CLASSES. */
+fs_status fs_logprobs_workspace(int64_t rows, int32_t classes, int32_t dtype, int32_t n_top, size_t *bytes);
+fs_status fs_logprobs(const void *d_scores, int64_t rows, int32_t classes, int64_t stride, int32_t dtype,
+                      float temperature, const int32_t *d_labels, int32_t n_top, float *d_logp, float *d_entropy,
+                      float *d_norm, int32_t *d_top_id, float *d_top_logp, void *d_workspace,
+                      size_t workspace_bytes, void *stream);
+
+/* Gradient of fs_logprobs with respect to the scores: for every row
+ *   g_j = (g_logp ([j = label] - p_j) - g_entropy p_j (ln p_j + entropy)) / T
+ * from the same scores, labels and temperature, fs_logprobs' d_norm, and the
+ * gradients of its outputs d_g_logp [rows] (needs d_labels) and d_g_entropy
+ * [rows] (needs d_entropy, fs_logprobs' own); either may be NULL, not both.
+ * Rows without a label take no part of d_g_logp; rows of nothing but -inf
+ * have gradient 0; rows of NaN or +inf, and rows whose label is >= classes
+ * when d_g_logp is given, NaN.  d_g_scores may be d_scores itself with the
+ * same stride. */
+fs_status fs_logprobs_grad(const void *d_scores, int64_t rows, int32_t classes, int64_t stride, int32_t dtype,
+                           float temperature, const int32_t *d_labels, const float *d_norm, const float *d_entropy,
+                           const float *d_g_logp, const float *d_g_entropy, void *d_g_scores, int64_t g_stride,
+                           void *stream);
+
+/* A fully connected layer on rows, shared by all of them, with a low-rank
+ * adapter of each row's own choice beside it:
+ *   y = W x + bias + s_i B_i (A_i x),   i = d_ids[row]
+ * A negative i leaves the adapter out; i >= n_adapters gives a row of NaN.
+ * d_w [m][k] with w_stride elements between its rows (a 1 x 1 layer's OIHW
+ * weights); d_bias float [m] or NULL; d_a [n_adapters][rank][k] and d_b
+ * [n_adapters][m][rank], contiguous; d_scale float [n_adapters] or NULL for
+ * ones; d_ids int32 [rows].  n_adapters = 0: no adapters, rank 0, the factor
+ * and id pointers NULL. */
+typedef struct {
+    int64_t rows;
+    int32_t k;
+    int32_t m;
+    int32_t dtype;
+    int32_t n_adapters;
+    int32_t rank;
+    const void *d_x;
+    int64_t x_stride;
+    const void *d_w;
+    int64_t w_stride;
+    const float *d_bias;
+    const void *d_a;
+    const void *d_b;
+    const float *d_scale;
+    const int32_t *d_ids;
+} fs_projection;
+
+/* d_y [rows][m] of dtype, y_stride elements between rows.  d_hidden, float
+ * [rows][rank] contiguous or NULL: A_i x of each row (0 for rows without an
+ * adapter, NaN where y is), which fs_project_grad takes back. */
+fs_status fs_project_workspace(const fs_projection *p, size_t *bytes);
+fs_status fs_project(const fs_projection *p, void *d_y, int64_t y_stride, float *d_hidden, void *d_workspace,
+                     size_t workspace_bytes, void *stream);
+
+/* Gradients of fs_project for given d_g [rows][m] (dtype, g_stride), W and the
+ * scales being constants: with u = s_i B_i^T g,
+ *   d_gx [rows][k] (dtype, gx_stride; or NULL): W^T g + A_i^T u
+ *   d_ga [n_adapters][rank][k], d_gb [n_adapters][m][rank] (dtype; both or
+ *   neither): sums over the adapter's rows of u x^T and of s_i g (A_i x)^T,
+ *   zero for an adapter that no row names.
+ * d_hidden: fs_project's, or NULL to compute it again.  Rows whose id is >=
+ * n_adapters get NaN in d_gx and take no part in d_ga and d_gb.  Sums over
+ * rows are taken in an order fixed by the sizes: the same bits every time. */
+fs_status fs_project_grad_workspace(const fs_projection *p, size_t *bytes);
+fs_status fs_project_grad(const fs_projection *p, const void *d_g, int64_t g_stride, const float *d_hidden,
+                          void *d_gx, int64_t gx_stride, void *d_ga, void *d_gb, void *d_workspace,
+                          size_t workspace_bytes, void *stream);
+
 const char *fs_status_str(fs_status s);
 const char *fs_last_error(void);
 

@@ -1599,6 +1599,11 @@ hipError_t enqueue(const fs_net *net, const Plan &P, const float *d_image, float
 
 }  // namespace
 
+// The row operators' entry points (rows_api.hip) report through the same message.
+namespace fs {
+int row_error(int status, const char *msg) { return fail((fs_status)status, "%s", msg); }
+}  // namespace fs
+
 // ---------------------------------------------------------------------------
 // C-ABI
 // ---------------------------------------------------------------------------

@@ -1,0 +1,71 @@
+// Internal declarations of the row operators (fs_logprobs, fs_project and
+// their gradients): launch arguments, and the conversions their kernels share.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "fs_internal.h"
+
+namespace fs {
+
+// The thread-local message behind fs_last_error (api.hip); returns `status`.
+int row_error(int status, const char *msg);
+
+struct LogprobArgs {
+    const void *x;          // [rows][V], stride elements apart
+    int64_t rows, stride;
+    int V;
+    float inv_t;            // 1 / temperature
+    const int *labels;      // [rows] or null
+    int n_top;
+    float *logp, *entropy;  // [rows] or null
+    float *norm;            // [rows][2] or null
+    int *top_id;            // [rows][n_top] or null
+    float *top_logp;        // [rows][n_top] or null
+};
+
+struct LogprobGradArgs {
+    const void *x;
+    int64_t rows, stride;
+    int V;
+    float inv_t;
+    const int *labels;
+    const float *norm, *entropy, *g_logp, *g_entropy;
+    void *g;                // [rows][V], g_stride apart
+    int64_t g_stride;
+};
+
+struct ProjArgs {
+    int64_t rows;
+    int K, M, n, r;         // inputs, outputs, adapters, rank
+    const void *x, *w;
+    int64_t xs, ws;         // row strides
+    const float *bias;      // or null
+    const void *a, *b;      // [n][r][K], [n][M][r]
+    const float *scale;     // [n] or null
+    const int *ids;         // [rows], null when n == 0
+};
+
+size_t logprobs_workspace(int64_t rows, int V, int dtype, int n_top);
+hipError_t launch_logprobs(const LogprobArgs &a, int dtype, void *ws, hipStream_t s);
+hipError_t launch_logprobs_grad(const LogprobGradArgs &a, int dtype, hipStream_t s);
+size_t project_workspace(const ProjArgs &a, int dtype);
+hipError_t launch_project(const ProjArgs &a, int dtype, void *y, int64_t ys, float *hidden, void *ws, hipStream_t s);
+size_t project_grad_workspace(const ProjArgs &a, int dtype);
+hipError_t launch_project_grad(const ProjArgs &a, int dtype, const void *g, int64_t gs, const float *hidden, void *gx,
+                               int64_t gxs, void *ga, void *gb, void *ws, hipStream_t s);
+
+__device__ __forceinline__ float to_f32(float v) { return v; }
+__device__ __forceinline__ float to_f32(uint16_t v) { return __uint_as_float((uint32_t)v << 16); }
+// bf16, round to nearest even; a NaN keeps its sign and becomes quiet
+__device__ __forceinline__ uint16_t to_bf16(float f)
+{
+    const uint32_t u = __float_as_uint(f);
+    if ((u & 0x7fffffffu) > 0x7f800000u) return (uint16_t)((u >> 16) | 0x40);
+    return (uint16_t)((u + 0x7fffu + ((u >> 16) & 1)) >> 16);
+}
+__device__ __forceinline__ void store_as(float *p, float v) { *p = v; }
+__device__ __forceinline__ void store_as(uint16_t *p, float v) { *p = to_bf16(v); }
+
+}  // namespace fs

@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+from collections import namedtuple
 
 import numpy as np
 
@@ -49,6 +50,14 @@ class fs_plan_info(ctypes.Structure):
                 ("flops", ctypes.c_double), ("min_bytes", ctypes.c_double)]
 
 
+class fs_projection(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("k", ctypes.c_int32), ("m", ctypes.c_int32), ("dtype", ctypes.c_int32),
+                ("n_adapters", ctypes.c_int32), ("rank", ctypes.c_int32), ("d_x", ctypes.c_void_p),
+                ("x_stride", ctypes.c_int64), ("d_w", ctypes.c_void_p), ("w_stride", ctypes.c_int64),
+                ("d_bias", ctypes.c_void_p), ("d_a", ctypes.c_void_p), ("d_b", ctypes.c_void_p),
+                ("d_scale", ctypes.c_void_p), ("d_ids", ctypes.c_void_p)]
+
+
 class fs_launch_info(ctypes.Structure):
     _fields_ = [("layer", ctypes.c_int32), ("n_layers", ctypes.c_int32), ("kind", ctypes.c_int32),
                 ("fragments", ctypes.c_int32), ("out_pixels", ctypes.c_int64),
@@ -60,7 +69,8 @@ class fs_launch_info(ctypes.Structure):
 EXPORTS = ["fs_net_create", "fs_net_create_plan_only", "fs_net_destroy", "fs_net_query", "fs_scan_plan", "fs_scan_launches",
            "fs_scan", "fs_scan_profile", "fs_fragment_table", "fs_reassembly_index",
            "fs_status_str", "fs_last_error", "fs_scan_plan_border", "fs_scan_border",
-           "fs_scan_plan_tiled", "fs_scan_tiled", "fs_scan_noalloc"]
+           "fs_scan_plan_tiled", "fs_scan_tiled", "fs_scan_noalloc", "fs_logprobs_workspace", "fs_logprobs",
+           "fs_logprobs_grad", "fs_project_workspace", "fs_project", "fs_project_grad_workspace", "fs_project_grad"]
 
 _libs = {}
 
@@ -76,6 +86,7 @@ def load(debug=False):
                            "python paper_1302_1700_amd/build.py" % path)
     lib = ctypes.CDLL(path)
     P, I32, SZ, VP = ctypes.POINTER, ctypes.c_int32, ctypes.c_size_t, ctypes.c_void_p
+    I64, F32 = ctypes.c_int64, ctypes.c_float
     sig = {
         "fs_net_create": [P(fs_layer), I32, I32, I32, I32, P(VP)],
         "fs_net_create_plan_only": [P(fs_layer), I32, I32, I32, I32, P(VP)],
@@ -92,6 +103,13 @@ def load(debug=False):
         "fs_scan_profile": [VP, VP, I32, I32, I32, VP, VP, SZ, VP, I32, P(ctypes.c_float), I32],
         "fs_fragment_table": [VP, I32, I32, P(I32), SZ, P(SZ)],
         "fs_reassembly_index": [VP, I32, I32, P(I32), SZ, P(SZ)],
+        "fs_logprobs_workspace": [I64, I32, I32, I32, P(SZ)],
+        "fs_logprobs": [VP, I64, I32, I64, I32, F32, VP, I32, VP, VP, VP, VP, VP, VP, SZ, VP],
+        "fs_logprobs_grad": [VP, I64, I32, I64, I32, F32, VP, VP, VP, VP, VP, VP, I64, VP],
+        "fs_project_workspace": [P(fs_projection), P(SZ)],
+        "fs_project": [P(fs_projection), VP, I64, VP, VP, SZ, VP],
+        "fs_project_grad_workspace": [P(fs_projection), P(SZ)],
+        "fs_project_grad": [P(fs_projection), VP, I64, VP, VP, I64, VP, VP, VP, SZ, VP],
         "fs_status_str": [ctypes.c_int],
         "fs_last_error": [],
     }
@@ -342,3 +360,239 @@ class Net:
                                          ctypes.c_void_p(out.data_ptr()), ctypes.c_void_p(ws.data_ptr()),
                                          _nbytes(ws), _stream_handle(stream), reps, ms, n), self._lib)
         return list(ms)
+
+
+# -- rows ------------------------------------------------------------------------
+LogProbs = namedtuple("LogProbs", "logp entropy norm top_id top_logp")
+LogProbs.__doc__ = """What logprobs returns, for scores [..., classes]: logp [...] (None without labels), entropy
+[...], norm [..., 2] = (largest score, log of the sum of exponentials relative to it), top_id and top_logp
+[..., n_top] (None with n_top 0)."""
+
+Adapters = namedtuple("Adapters", "a b scale", defaults=(None,))
+Adapters.__doc__ = """Low-rank adapters of a projection k -> m: a [n, rank, k], b [n, m, rank] (the projection's
+dtype, contiguous), scale float32 [n] or None for ones; adapter i adds scale_i b_i (a_i x)."""
+
+
+def _row_dtype(t, name):
+    import torch
+    if t.dtype == torch.float32:
+        return 0
+    if t.dtype == torch.bfloat16:
+        return 1
+    raise ValueError("%s must be float32 or bfloat16" % name)
+
+
+def _rows_of(t, name):
+    """(rows, row length, row stride) of [..., length] read as rows; its rows
+    must lie at one stride, the elements of a row side by side."""
+    if t.dim() < 1:
+        raise ValueError("%s must have a last dimension" % name)
+    n = t.shape[-1]
+    if n < 1:
+        raise ValueError("%s has rows of no elements" % name)
+    if n > 1 and t.stride(-1) != 1:
+        raise ValueError("the elements of a row of %s must be adjacent" % name)
+    rows = t.numel() // n
+    stride = n
+    if rows > 1 and not t.is_contiguous():
+        dims = [(d, s) for d, s in zip(t.shape[:-1], t.stride()[:-1]) if d > 1]
+        stride = dims[-1][1]
+        step = stride
+        for d, s in reversed(dims):
+            if s != step:
+                raise ValueError("the rows of %s do not lie at one stride" % name)
+            step = s * d
+    return rows, n, stride
+
+
+def _row_array(t, name, dtype, shape, device):
+    """A given index, statistic or output array: dense, of this type and shape."""
+    if t.dtype != dtype or tuple(t.shape) != tuple(shape) or not t.is_contiguous() or t.device != device:
+        raise ValueError("%s must be a contiguous %s tensor %s on %s" % (name, str(dtype)[6:], tuple(shape), device))
+    return t.data_ptr()
+
+
+def _row_out(t, name, like, shape):
+    """A given or new output of rows, and its row stride."""
+    import torch
+    if t is None:
+        return torch.empty(shape, dtype=like.dtype, device=like.device), shape[-1]
+    if t.dtype != like.dtype or tuple(t.shape) != tuple(shape) or t.device != like.device:
+        raise ValueError("%s must be a %s tensor %s on %s" % (name, str(like.dtype)[6:], tuple(shape), like.device))
+    return t, _rows_of(t, name)[2]
+
+
+class _On:
+    """The device and stream of a call: the tensors' device is made the current
+    one if it is not, and what the call allocates belongs to its stream."""
+
+    def __init__(self, t, stream):
+        import torch
+        if not t.is_cuda:
+            raise ValueError("the tensors must be on a GPU")
+        if stream is not None and stream.device != t.device:
+            raise ValueError("the stream is on %s, the tensors on %s" % (stream.device, t.device))
+        self._in = []
+        if torch.cuda.current_device() != t.device.index:
+            self._in.append(torch.cuda.device(t.device))
+        if stream is not None:
+            self._in.append(torch.cuda.stream(stream))
+
+    def __enter__(self):
+        import torch
+        for c in self._in:
+            c.__enter__()
+        return torch.cuda.current_stream().cuda_stream
+
+    def __exit__(self, *exc):
+        for c in reversed(self._in):
+            c.__exit__(*exc)
+        return False
+
+
+def _row_workspace(nbytes, given, device):
+    import torch
+    if given is not None:
+        if not given.is_contiguous() or given.device != device:
+            raise ValueError("workspace must be contiguous and on %s" % device)
+        return given, _nbytes(given)
+    if not nbytes:
+        return None, 0
+    return torch.empty(nbytes, dtype=torch.uint8, device=device), nbytes
+
+
+def _ptr(t):
+    return None if t is None else t.data_ptr()
+
+
+def logprobs(scores, labels=None, n_top=0, temperature=1.0, workspace=None, stream=None):
+    """Log probabilities of the labels, entropy and the n_top best classes of
+    rows of scores (fs_logprobs): scores [..., classes] float32 or bfloat16,
+    labels int32 [...] (negative: none) -> LogProbs."""
+    import torch
+    lib = load()
+    dt = _row_dtype(scores, "scores")
+    rows, V, stride = _rows_of(scores, "scores")
+    shape, dev = scores.shape[:-1], scores.device
+    n_top = int(n_top)
+    if labels is not None:
+        _row_array(labels, "labels", torch.int32, shape, dev)
+    with _On(scores, stream) as s:
+        need = ctypes.c_size_t()
+        _check(lib.fs_logprobs_workspace(rows, V, dt, n_top, ctypes.byref(need)), lib)
+        ws, have = _row_workspace(need.value, workspace, dev)
+        f32 = dict(dtype=torch.float32, device=dev)
+        logp = torch.empty(shape, **f32) if labels is not None else None
+        entropy = torch.empty(shape, **f32)
+        norm = torch.empty((*shape, 2), **f32)
+        top_id = torch.empty((*shape, n_top), dtype=torch.int32, device=dev) if n_top else None
+        top_logp = torch.empty((*shape, n_top), **f32) if n_top else None
+        _check(lib.fs_logprobs(scores.data_ptr(), rows, V, stride, dt, float(temperature), _ptr(labels), n_top,
+                               _ptr(logp), entropy.data_ptr(), norm.data_ptr(), _ptr(top_id), _ptr(top_logp),
+                               _ptr(ws), have, s), lib)
+    return LogProbs(logp, entropy, norm, top_id, top_logp)
+
+
+def logprobs_grad(scores, norm, labels=None, g_logp=None, entropy=None, g_entropy=None, temperature=1.0, out=None,
+                  stream=None):
+    """Gradient of logprobs with respect to the scores (fs_logprobs_grad) from
+    its norm (and entropy), and the gradients g_logp [...] of its logp and
+    g_entropy [...] of its entropy (either may be None).  `out` may be the
+    scores themselves."""
+    import torch
+    lib = load()
+    dt = _row_dtype(scores, "scores")
+    rows, V, stride = _rows_of(scores, "scores")
+    shape, dev = scores.shape[:-1], scores.device
+    given = [_row_array(norm, "norm", torch.float32, (*shape, 2), dev)]
+    for t, name, kind in ((labels, "labels", torch.int32), (entropy, "entropy", torch.float32),
+                          (g_logp, "g_logp", torch.float32), (g_entropy, "g_entropy", torch.float32)):
+        given.append(None if t is None else _row_array(t, name, kind, shape, dev))
+    norm_p, labels_p, entropy_p, g_logp_p, g_entropy_p = given
+    with _On(scores, stream) as s:
+        out, g_stride = _row_out(out, "out", scores, tuple(scores.shape))
+        _check(lib.fs_logprobs_grad(scores.data_ptr(), rows, V, stride, dt, float(temperature), labels_p, norm_p,
+                                    entropy_p, g_logp_p, g_entropy_p, out.data_ptr(), g_stride, s), lib)
+    return out
+
+
+def _projection(x, weight, bias, adapters, ids):
+    import torch
+    dt = _row_dtype(x, "x")
+    rows, K, stride = _rows_of(x, "x")
+    dev = x.device
+    if weight.dim() != 2 or weight.shape[1] != K or weight.dtype != x.dtype or weight.device != dev:
+        raise ValueError("weight must be a %s tensor [m, %d] on %s" % (str(x.dtype)[6:], K, dev))
+    M, _, w_stride = _rows_of(weight, "weight")
+    p = fs_projection(rows=rows, k=K, m=M, dtype=dt, d_x=x.data_ptr(), x_stride=stride, d_w=weight.data_ptr(),
+                      w_stride=w_stride)
+    if bias is not None:
+        p.d_bias = _row_array(bias, "bias", torch.float32, (M,), dev)
+    if adapters is not None:
+        a, b, scale = adapters
+        if a.dim() != 3 or b.dim() != 3 or a.shape[0] < 1 or a.shape[1] < 1:
+            raise ValueError("adapters must be a [n, rank, k] and b [n, m, rank], neither empty")
+        n, r = a.shape[:2]
+        p.n_adapters, p.rank = n, r
+        p.d_a = _row_array(a, "adapters' a", x.dtype, (n, r, K), dev)
+        p.d_b = _row_array(b, "adapters' b", x.dtype, (n, M, r), dev)
+        if scale is not None:
+            p.d_scale = _row_array(scale, "adapters' scale", torch.float32, (n,), dev)
+        if ids is None:
+            raise ValueError("adapters need ids")
+        p.d_ids = _row_array(ids, "ids", torch.int32, x.shape[:-1], dev)
+    elif ids is not None:
+        raise ValueError("ids without adapters")
+    return p
+
+
+def project(x, weight, bias=None, adapters=None, ids=None, out=None, return_hidden=False, workspace=None, stream=None):
+    """Rows through a shared fully connected layer, each with the adapter it
+    names beside it (fs_project): x [..., k], weight [m, k] of one dtype, bias
+    float32 [m], adapters an Adapters, ids int32 [...] (negative: none) ->
+    [..., m], with return_hidden also a_i x [..., rank] float32, which
+    project_grad takes back."""
+    import torch
+    lib = load()
+    p = _projection(x, weight, bias, adapters, ids)
+    if return_hidden and adapters is None:
+        raise ValueError("return_hidden without adapters")
+    with _On(x, stream) as s:
+        need = ctypes.c_size_t()
+        _check(lib.fs_project_workspace(ctypes.byref(p), ctypes.byref(need)), lib)
+        ws, have = _row_workspace(need.value, workspace, x.device)
+        out, y_stride = _row_out(out, "out", x, (*x.shape[:-1], p.m))
+        hidden = torch.empty((*x.shape[:-1], p.rank), dtype=torch.float32, device=x.device) if return_hidden else None
+        _check(lib.fs_project(ctypes.byref(p), out.data_ptr(), y_stride, _ptr(hidden), _ptr(ws), have, s), lib)
+    return (out, hidden) if return_hidden else out
+
+
+def project_grad(g, x, weight, adapters=None, ids=None, hidden=None, need_x=True, need_adapters=True, workspace=None,
+                 stream=None):
+    """Gradients of project for the gradient g [..., m] of its output, the
+    weight and scales being constants (fs_project_grad) -> (g_x, g_a, g_b), None
+    for those not wanted; hidden: project's, or None to compute it again."""
+    import torch
+    lib = load()
+    p = _projection(x, weight, None, adapters, ids)
+    if g.dtype != x.dtype or tuple(g.shape) != (*x.shape[:-1], p.m) or g.device != x.device:
+        raise ValueError("g must be a %s tensor %s on %s" % (str(x.dtype)[6:], (*x.shape[:-1], p.m), x.device))
+    g_stride = _rows_of(g, "g")[2]
+    need_adapters = need_adapters and adapters is not None
+    if not need_x and not need_adapters:
+        raise ValueError("no gradient is wanted")
+    h = None
+    if hidden is not None:
+        if adapters is None:
+            raise ValueError("hidden without adapters")
+        h = _row_array(hidden, "hidden", torch.float32, (*x.shape[:-1], p.rank), x.device)
+    with _On(x, stream) as s:
+        need = ctypes.c_size_t()
+        _check(lib.fs_project_grad_workspace(ctypes.byref(p), ctypes.byref(need)), lib)
+        ws, have = _row_workspace(need.value, workspace, x.device)
+        gx = torch.empty(x.shape, dtype=x.dtype, device=x.device) if need_x else None
+        ga = torch.empty_like(adapters.a) if need_adapters else None
+        gb = torch.empty_like(adapters.b) if need_adapters else None
+        _check(lib.fs_project_grad(ctypes.byref(p), g.data_ptr(), g_stride, h, _ptr(gx), p.k, _ptr(ga), _ptr(gb),
+                                   _ptr(ws), have, s), lib)
+    return gx, ga, gb
