@@ -398,8 +398,7 @@ fs_status fs_reassembly_index(const fs_net *net, int32_t H, int32_t W, int32_t *
  * 0), entropy 0, log probability -inf for every label and an empty list.  A
  * row that holds a NaN or +inf gives NaN throughout and -1 in its list.
  * Any output may be NULL if another is not; d_logp needs d_labels.
- * FS_ERR_INVALID_ARG for a temperature that is not above 0 or whose inverse
- * is not finite, n_top outside 0 .. FS_MAX_TOP, classes outside 1 ..
+ * FS_ERR_INVALID_ARG for a temperature outside 1e-30 .. 1e30, n_top outside 0 .. FS_MAX_TOP, classes outside 1 ..
  * FS_MAX_CLASSES. */
 fs_status fs_logprobs_workspace(int64_t rows, int32_t classes, int32_t dtype, int32_t n_top, size_t *bytes);
 fs_status fs_logprobs(const void *d_scores, int64_t rows, int32_t classes, int64_t stride, int32_t dtype,

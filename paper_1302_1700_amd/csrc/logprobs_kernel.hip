@@ -3,14 +3,42 @@
 //
 // With m the row's maximum, d_j = (x_j - m) / T <= 0, S = sum exp(d_j) and
 // D = sum exp(d_j) d_j: log p_j = d_j - ln S and the entropy is ln S - D / S,
-// two terms >= 0, so nothing cancels where the scores are far from 0.
-// One wave per row, lanes striding over the classes.
+// two terms >= 0, so nothing cancels where the scores are far from 0.  The
+// kernels keep d in units of log2 (one factor k = log2(e) / T, the hardware's
+// exp2) and D with it.  Every row is read once.
+//
+// A score of -inf has exp 0; its d is held at -1e30 where it multiplies that 0.
+// Maxima start from the lowest finite float, so -inf never meets -inf; S = 0
+// then says that a row is empty, and a NaN or +inf makes S a NaN by itself.
 #include <algorithm>
+#include <type_traits>
 
 #include "rows.h"
 
 namespace fs {
 namespace {
+
+constexpr float kLowest = -3.402823466e38f;
+constexpr float kLog2e = 1.44269504088896f, kLn2 = 0.693147180559945f;
+constexpr float kFar = -1e30f;
+
+// Elements per 16-byte load, and the load itself: rows start anywhere their
+// element type may, and the memory pipeline takes such addresses.
+template <typename T>
+constexpr int kVec = 16 / sizeof(T);
+
+template <typename T, int N>
+struct __attribute__((packed, aligned(alignof(T)))) Run {
+    T v[N];
+};
+
+template <typename T, int N>
+__device__ __forceinline__ void load_run(const T *p, float *v)
+{
+    const Run<T, N> r = *reinterpret_cast<const Run<T, N> *>(p);
+#pragma unroll
+    for (int e = 0; e < N; ++e) v[e] = to_f32(r.v[e]);
+}
 
 // Scores in the order of their values, equal ones by their class: the float as
 // an unsigned number that compares alike (-0 as 0), then the class reversed.
@@ -28,129 +56,599 @@ __device__ __forceinline__ float key_score(uint64_t k)
 }
 __device__ __forceinline__ int key_id(uint64_t k) { return (int)(0xffffffffu - (uint32_t)k); }
 
-template <typename T>
-__device__ __forceinline__ T wave_max(T v)
+template <int G, typename T>
+__device__ __forceinline__ T group_max(T v)
 {
 #pragma unroll
-    for (int d = 32; d; d >>= 1) {
+    for (int d = G / 2; d; d >>= 1) {
         const T o = __shfl_xor(v, d);
         v = o > v ? o : v;
     }
     return v;
 }
-__device__ __forceinline__ float wave_sum(float v)
+template <int G>
+__device__ __forceinline__ float group_sum(float v)
 {
 #pragma unroll
-    for (int d = 32; d; d >>= 1) v += __shfl_xor(v, d);
+    for (int d = G / 2; d; d >>= 1) v += __shfl_xor(v, d);
     return v;
 }
 
-template <typename T>
-__global__ __launch_bounds__(256) void logprobs_row(LogprobArgs a)
+// What is known of a part of a row: maximum, S and D relative to it.
+struct Part {
+    float m, s, d;
+};
+
+// A part seen from a larger maximum.
+__device__ __forceinline__ void move_to(Part &p, float m, float k)
 {
-    const int lane = threadIdx.x & 63;
-    for (int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); row < a.rows; row += (int64_t)gridDim.x * 4) {
+    const float t = fmaxf((p.m - m) * k, kFar);
+    const float c = __builtin_amdgcn_exp2f(t);
+    p.d = c * fmaf(p.s, t, p.d);
+    p.s *= c;
+    p.m = m;
+}
+
+template <int G>
+__device__ __forceinline__ Part group_join(Part p, float k)
+{
+    move_to(p, group_max<G>(p.m), k);
+    p.s = group_sum<G>(p.s);
+    p.d = group_sum<G>(p.d);
+    return p;
+}
+
+// A row's statistics as they are stored.
+struct RowStats {
+    float m, log_s, entropy;
+    bool bad, empty;
+};
+
+__device__ __forceinline__ RowStats finish(const Part &p)
+{
+    RowStats r;
+    r.bad = !(p.s >= 0.f);
+    r.empty = p.s == 0.f;
+    r.m = r.bad ? NAN : r.empty ? -INFINITY : p.m;
+    r.log_s = r.bad ? NAN : r.empty ? 0.f : logf(p.s);
+    r.entropy = r.bad ? NAN : r.empty ? 0.f : r.log_s - p.d * kLn2 / p.s;
+    return r;
+}
+
+__device__ __forceinline__ float label_logp(const RowStats &r, int y, int V, float xy, float inv_t)
+{
+    if (y < 0) return 0.f;
+    if (y >= V || r.bad) return NAN;
+    return r.empty ? -INFINITY : (xy - r.m) * inv_t - r.log_s;
+}
+
+__device__ __forceinline__ void store_stats(const LogprobArgs &a, int64_t row, const RowStats &r, int y, float xy)
+{
+    if (a.norm) *reinterpret_cast<Run<float, 2> *>(a.norm + 2 * row) = Run<float, 2>{{r.m, r.log_s}};
+    if (a.entropy) a.entropy[row] = r.entropy;
+    if (a.logp) a.logp[row] = label_logp(r, y, a.V, xy, a.inv_t);
+}
+
+__device__ __forceinline__ void store_top(const LogprobArgs &a, int64_t row, int place, const RowStats &r, uint64_t key)
+{
+    const bool none = r.bad || key == 0;
+    if (a.top_id) a.top_id[row * a.n_top + place] = none ? -1 : key_id(key);
+    if (a.top_logp)
+        a.top_logp[row * a.n_top + place] =
+            r.bad ? NAN : none ? -INFINITY : (key_score(key) - r.m) * a.inv_t - r.log_s;
+}
+
+// Short rows: G lanes hold a row in registers, C chunks of N scores each (lane
+// l of the group: chunks l, l + G, ...), 64 / G rows a wave.  The best classes
+// are taken out one after the other, a group maximum each.
+template <typename T, int G, int C, int N>
+__global__ __launch_bounds__(256) void logprobs_short(LogprobArgs a)
+{
+    const int sub = threadIdx.x % G;
+    const int V = a.V;
+    const float k = a.inv_t * kLog2e;
+    for (int64_t row = (int64_t)blockIdx.x * (256 / G) + threadIdx.x / G; row < a.rows;
+         row += (int64_t)gridDim.x * (256 / G)) {
         const T *x = reinterpret_cast<const T *>(a.x) + row * a.stride;
-        float m = -INFINITY;
-        bool bad = false;  // NaN or +inf
-        for (int j = lane; j < a.V; j += 64) {
-            const float v = to_f32(x[j]);
-            bad |= !(v < INFINITY);
-            m = fmaxf(m, v);
-        }
-        m = wave_max(m);
-        bad = __any(bad);
-        const bool empty = m == -INFINITY;
-        float s = 0.f, d = 0.f;
-        for (int j = lane; j < a.V; j += 64) {
-            const float t = empty ? -INFINITY : (to_f32(x[j]) - m) * a.inv_t;
-            const float e = expf(t);
-            s += e;
-            d += e * fmaxf(t, -1e30f);  // a class ruled out: 0, not 0 * inf
-        }
-        s = wave_sum(s);
-        d = wave_sum(d);
-        float log_s = empty ? 0.f : logf(s), ent = empty ? 0.f : log_s - d / s;
-        if (bad) m = log_s = ent = NAN;
-        if (lane == 0) {
-            if (a.norm) {
-                a.norm[2 * row] = m;
-                a.norm[2 * row + 1] = log_s;
-            }
-            if (a.entropy) a.entropy[row] = ent;
-            if (a.logp) {
-                const int y = a.labels[row];
-                float lp = 0.f;
-                if (y >= a.V) lp = NAN;
-                else if (y >= 0) lp = bad ? NAN : empty ? -INFINITY : (to_f32(x[y]) - m) * a.inv_t - log_s;
-                a.logp[row] = lp;
+        const int y = a.logp ? a.labels[row] : -1;
+        float v[C * N];
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            const int j = (c * G + sub) * N;
+            if (j + N <= V) load_run<T, N>(x + j, v + c * N);
+            else {
+#pragma unroll
+                for (int e = 0; e < N; ++e) v[c * N + e] = j + e < V ? to_f32(x[j + e]) : -INFINITY;
             }
         }
-        uint64_t last = ~0ull;  // the class listed before
-        for (int t = 0; t < a.n_top; ++t) {
+        const float xy = y >= 0 && y < V ? to_f32(x[y]) : 0.f;
+        Part p{kLowest, 0.f, 0.f};
+#pragma unroll
+        for (int e = 0; e < C * N; ++e) p.m = fmaxf(p.m, v[e]);
+        p.m = group_max<G>(p.m);
+#pragma unroll
+        for (int e = 0; e < C * N; ++e) {
+            const float t = (v[e] - p.m) * k, w = __builtin_amdgcn_exp2f(t);
+            p.s += w;
+            p.d = fmaf(w, fmaxf(t, kFar), p.d);
+        }
+        p.s = group_sum<G>(p.s);
+        p.d = group_sum<G>(p.d);
+        const RowStats r = finish(p);
+        if (sub == 0) store_stats(a, row, r, y, xy);
+        for (int place = 0; place < a.n_top; ++place) {
             uint64_t best = 0;
-            if (!bad && last) {
-                for (int j = lane; j < a.V; j += 64) {
-                    const float v = to_f32(x[j]);
-                    const uint64_t k = v == -INFINITY ? 0 : score_key(v, (uint32_t)j);
-                    if (k < last && k > best) best = k;
-                }
-                best = wave_max(best);
+#pragma unroll
+            for (int e = 0; e < C * N; ++e) {
+                const uint64_t key = score_key(v[e], (uint32_t)((e / N * G + sub) * N + e % N));
+                if (v[e] != -INFINITY && key > best) best = key;
             }
-            last = best;
-            if (lane == 0) {
-                if (a.top_id) a.top_id[row * a.n_top + t] = best ? key_id(best) : -1;
-                if (a.top_logp)
-                    a.top_logp[row * a.n_top + t] =
-                        bad ? NAN : best ? (key_score(best) - m) * a.inv_t - log_s : -INFINITY;
+            best = group_max<G>(best);
+            if (sub == 0) store_top(a, row, place, r, best);
+            const int id = best ? key_id(best) : -1;
+#pragma unroll
+            for (int e = 0; e < C * N; ++e)
+                if ((e / N * G + sub) * N + e % N == id) v[e] = -INFINITY;
+        }
+    }
+}
+
+// The n best scores so far, best first, one in each of the wave's lanes.
+// A new score goes in behind its equals (scores come in the order of their
+// classes): the lanes from its place on take over from the lane before.
+struct Best {
+    float v;
+    int id;
+    __device__ __forceinline__ void insert(float nv, int nid, int lane)
+    {
+        const int place = __popcll(__ballot(v >= nv));
+        const float uv = __shfl_up(v, 1);
+        const int uid = __shfl_up(id, 1);
+        v = lane < place ? v : lane == place ? nv : uv;
+        id = lane < place ? id : lane == place ? nid : uid;
+    }
+};
+
+__device__ __forceinline__ float lane_value(float v, int lane)
+{
+    return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v), lane));
+}
+
+// The n-th largest of the wave's values (n <= 64).
+__device__ __forceinline__ float nth_largest(float v, int n, int lane)
+{
+    int before = 0;
+#pragma unroll
+    for (int o = 0; o < 64; ++o) {
+        const float w = lane_value(v, o);
+        before += (w > v || (w == v && o < lane)) ? 1 : 0;
+    }
+    const uint64_t at = __ballot(before == n - 1);
+    return at ? lane_value(v, __ffsll((unsigned long long)at) - 1) : -INFINITY;  // none: NaNs among them
+}
+
+// The next float below v: "above it" is "at least v".
+__device__ __forceinline__ float just_below(float v)
+{
+    v += 0.0f;
+    const uint32_t u = __float_as_uint(v);
+    if (v == -INFINITY) return v;
+    return __uint_as_float(v > 0.f ? u - 1 : v < 0.f ? u + 1 : 0x80000001u);
+}
+
+// Joins sorted lists of n keys each (in LDS, `lists` of them, 0 past their
+// ends): a key's place is its own index plus the number of larger keys in each
+// other list.  Threads of the block take keys in turn; writes the n best.
+__device__ __forceinline__ void join_lists(const LogprobArgs &a, int64_t row, const RowStats &r, const uint64_t *keys,
+                                           int lists)
+{
+    const int n = a.n_top;
+    for (int q = threadIdx.x; q < lists * n; q += blockDim.x) {
+        const int mine = q / n;
+        const uint64_t key = keys[q];
+        int place = q - mine * n;
+        if (key == 0) {
+            // nobody's: the places behind all classes that are listed anywhere
+            if (mine != 0) continue;
+            for (int l = 1; l < lists; ++l) {
+                int lo = 0, hi = n;
+                while (lo < hi) {
+                    const int mid = (lo + hi) / 2;
+                    if (keys[l * n + mid] != 0) lo = mid + 1;
+                    else hi = mid;
+                }
+                place += lo;
+            }
+            if (place < n) store_top(a, row, place, r, 0);
+            continue;
+        }
+        for (int l = 0; l < lists && place < n; ++l) {
+            if (l == mine) continue;
+            int lo = 0, hi = n;
+            while (lo < hi) {
+                const int mid = (lo + hi) / 2;
+                if (keys[l * n + mid] > key) lo = mid + 1;
+                else hi = mid;
+            }
+            place += lo;
+        }
+        if (place < n) store_top(a, row, place, r, key);
+    }
+}
+
+// What a split of a row leaves for the join: its part, then its keys.
+__host__ __device__ __forceinline__ size_t split_bytes(int n_top) { return 16 + 8 * (size_t)n_top; }
+
+// Long rows: W waves to a row, or to one of `splits` runs of it, each going
+// through batches of kU * 64 * N scores, W batches apart, the next batch's
+// loads in flight.  A lane keeps its own maximum and sums, moved to the larger
+// maximum once a batch.  The best classes: a batch whose largest score in
+// every lane is at most the wave's n-th best adds nothing (one comparison and
+// a ballot); the first batch starts from the n-th largest of its lanes'
+// maxima, which at least n of its scores reach.
+constexpr int kU = 4;
+
+template <typename T, int W, bool TOP>
+__global__ __launch_bounds__(64 * W) void logprobs_long(LogprobArgs a, int splits, int per_split, char *parts)
+{
+    constexpr int N = kVec<T>, BATCH = kU * 64 * N;
+    extern __shared__ uint64_t lds_keys[];  // [W][n_top], when W > 1 and TOP
+    __shared__ Part lds_part[W];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const float k = a.inv_t * kLog2e;
+    const int n = TOP ? a.n_top : 0;
+    const int64_t units = a.rows * splits;
+    for (int64_t unit = blockIdx.x; unit < units; unit += gridDim.x) {
+        const int64_t row = splits == 1 ? unit : unit / splits;
+        const int first = (int)(unit - row * splits) * per_split;
+        const int V = min(a.V, first + per_split);  // this run's end
+        const T *x = reinterpret_cast<const T *>(a.x) + row * a.stride;
+        const int y = a.logp ? a.labels[row] : -1;
+        const float xy = y >= 0 && y < a.V ? to_f32(x[y]) : 0.f;
+
+        Part p{kLowest, 0.f, 0.f};
+        Best best{-INFINITY, -1};
+        float limit = -INFINITY;
+        bool started = false;
+        Run<T, N> next[kU];
+        auto fetch = [&](int at) {
+#pragma unroll
+            for (int u = 0; u < kU; ++u) {
+                const int j = at + (u * 64 + lane) * N;
+                if (j + N <= V) next[u] = *reinterpret_cast<const Run<T, N> *>(x + j);
+                else {
+#pragma unroll
+                    for (int e = 0; e < N; ++e) next[u].v[e] = j + e < V ? x[j + e] : (T)(sizeof(T) == 2 ? 0xff80 : 0);
+                    if constexpr (sizeof(T) == 4) {
+#pragma unroll
+                        for (int e = 0; e < N; ++e)
+                            if (j + e >= V) next[u].v[e] = -INFINITY;
+                    }
+                }
+            }
+        };
+        int at = first + wave * BATCH;
+        if (at < V) fetch(at);
+        for (; at < V; at += W * BATCH) {
+            float v[kU * N];
+#pragma unroll
+            for (int u = 0; u < kU; ++u)
+#pragma unroll
+                for (int e = 0; e < N; ++e) v[u * N + e] = to_f32(next[u].v[e]);
+            if (at + W * BATCH < V) fetch(at + W * BATCH);
+            float most[kU], high = -INFINITY;
+#pragma unroll
+            for (int u = 0; u < kU; ++u) {
+                most[u] = v[u * N];
+#pragma unroll
+                for (int e = 1; e < N; ++e) most[u] = fmaxf(most[u], v[u * N + e]);
+                high = fmaxf(high, most[u]);
+            }
+            move_to(p, fmaxf(p.m, high), k);
+#pragma unroll
+            for (int e = 0; e < kU * N; ++e) {
+                const float t = (v[e] - p.m) * k, w = __builtin_amdgcn_exp2f(t);
+                p.s += w;
+                p.d = fmaf(w, fmaxf(t, kFar), p.d);
+            }
+            if constexpr (TOP) {
+                if (!started) {
+                    started = true;
+                    limit = just_below(nth_largest(high, n, lane));
+                }
+                if (__ballot(high > limit)) {
+#pragma unroll
+                    for (int u = 0; u < kU; ++u) {
+                        uint64_t who = __ballot(most[u] > limit);
+                        while (who) {
+                            const int l = __ffsll((unsigned long long)who) - 1;
+#pragma unroll
+                            for (int e = 0; e < N; ++e) {
+                                const float nv = lane_value(v[u * N + e], l);
+                                if (nv > limit) {
+                                    best.insert(nv, at + (u * 64 + l) * N + e, lane);
+                                    limit = fmaxf(limit, lane_value(best.v, n - 1));
+                                }
+                            }
+                            who &= who - 1;
+                            who &= __ballot(most[u] > limit);
+                        }
+                    }
+                }
+            }
+        }
+        p = group_join<64>(p, k);
+        const uint64_t key = TOP && lane < n && best.v != -INFINITY ? score_key(best.v, (uint32_t)best.id) : 0;
+        if constexpr (W > 1) {
+            __syncthreads();  // the unit before has been read
+            if (lane == 0) lds_part[wave] = p;
+            if (TOP && lane < n) lds_keys[wave * n + lane] = key;
+            __syncthreads();
+            Part q{kLowest, 0.f, 0.f};
+            if (lane < W) q = lds_part[lane];
+            p = group_join<64>(q, k);
+        }
+        if (splits > 1) {
+            char *to = parts + unit * split_bytes(a.n_top);
+            if (threadIdx.x == 0) *reinterpret_cast<Part *>(to) = p;
+            if constexpr (TOP) {
+                uint64_t *out = reinterpret_cast<uint64_t *>(to + 16);
+                if constexpr (W == 1) {
+                    if (lane < n) out[lane] = key;
+                } else {
+                    // the waves' lists joined into one, as join_lists places them
+                    for (int q = threadIdx.x; q < n; q += 64 * W) out[q] = 0;
+                    __syncthreads();
+                    for (int q = threadIdx.x; q < W * n; q += 64 * W) {
+                        const int mine = q / n;
+                        const uint64_t ky = lds_keys[q];
+                        int place = q - mine * n;
+                        for (int l = 0; l < W && place < n && ky; ++l) {
+                            if (l == mine) continue;
+                            int lo = 0, hi = n;
+                            while (lo < hi) {
+                                const int mid = (lo + hi) / 2;
+                                if (lds_keys[l * n + mid] > ky) lo = mid + 1;
+                                else hi = mid;
+                            }
+                            place += lo;
+                        }
+                        if (ky && place < n) out[place] = ky;
+                    }
+                }
+            }
+            continue;
+        }
+        const RowStats r = finish(p);
+        if (threadIdx.x == 0) store_stats(a, row, r, y, xy);
+        if constexpr (TOP) {
+            if constexpr (W == 1) {
+                if (lane < n) store_top(a, row, lane, r, key);
+            } else {
+                join_lists(a, row, r, lds_keys, W);
             }
         }
     }
 }
 
+// Joins the splits of a row (at most 64).
 template <typename T>
-__global__ __launch_bounds__(256) void logprobs_grad_row(LogprobGradArgs a)
+__global__ __launch_bounds__(256) void logprobs_join(LogprobArgs a, int splits, const char *parts)
 {
-    const int lane = threadIdx.x & 63;
-    for (int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); row < a.rows; row += (int64_t)gridDim.x * 4) {
+    extern __shared__ uint64_t lds_keys[];  // [splits][n_top]
+    const float k = a.inv_t * kLog2e;
+    const int lane = threadIdx.x & 63, n = a.n_top;
+    for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+        const char *from = parts + row * splits * split_bytes(n);
+        Part p{kLowest, 0.f, 0.f};
+        if (lane < splits) p = *reinterpret_cast<const Part *>(from + lane * split_bytes(n));
+        __syncthreads();  // the row before has been read
+        for (int q = threadIdx.x; q < splits * n; q += 256)
+            lds_keys[q] = reinterpret_cast<const uint64_t *>(from + q / n * split_bytes(n) + 16)[q % n];
+        __syncthreads();
+        const RowStats r = finish(group_join<64>(p, k));
+        if (threadIdx.x == 0) {
+            const T *x = reinterpret_cast<const T *>(a.x) + row * a.stride;
+            const int y = a.logp ? a.labels[row] : -1;
+            store_stats(a, row, r, y, y >= 0 && y < a.V ? to_f32(x[y]) : 0.f);
+        }
+        if (n) join_lists(a, row, r, lds_keys, splits);
+    }
+}
+
+// -- gradient ------------------------------------------------------------------
+// exp with the product's rounding put back: p is off by its own rounding, not
+// by |ln p| times it
+__device__ __forceinline__ float exp_exact(float x)
+{
+    const float t = fmaxf(x, -200.f) * kLog2e;
+    const float rest = fmaf(fmaxf(x, -200.f), kLog2e, -t) + fmaxf(x, -200.f) * 1.925963033e-8f;
+    const float e = __builtin_amdgcn_exp2f(t);
+    return x != x ? x : fmaf(e, rest * kLn2, e);
+}
+
+// What the elements of a row's gradient share.
+struct GradRow {
+    float m, log_s, gl, ge, ent, inv_t;
+    int y;
+    bool zero;
+    __device__ __forceinline__ GradRow(const LogprobGradArgs &a, int64_t row)
+    {
+        const Run<float, 2> nm = *reinterpret_cast<const Run<float, 2> *>(a.norm + 2 * row);
+        y = a.labels ? a.labels[row] : -1;
+        gl = y >= 0 ? a.g_logp[row] : 0.f;
+        ge = a.g_entropy ? a.g_entropy[row] : 0.f;
+        ent = a.g_entropy ? a.entropy[row] : 0.f;
+        inv_t = a.inv_t;
+        m = y >= a.V ? NAN : nm.v[0];
+        log_s = nm.v[1];
+        zero = m == -INFINITY;
+    }
+    template <bool EXACT>
+    __device__ __forceinline__ float at(float x, int j) const
+    {
+        const float lp = (x - m) * inv_t - log_s;
+        const float p = EXACT ? exp_exact(lp) : __expf(lp);
+        const float v = gl * ((j == y ? 1.f : 0.f) - p) - ge * p * (fmaxf(lp, kFar) + ent);
+        return zero ? 0.f : v * inv_t;
+    }
+};
+
+template <typename T, int N>
+__device__ __forceinline__ void grad_run(const GradRow &r, const T *x, T *g, int j, int V)
+{
+    if (j + N <= V) {
+        float v[N];
+        load_run<T, N>(x + j, v);
+        Run<T, N> out;
+#pragma unroll
+        for (int e = 0; e < N; ++e) store_as(&out.v[e], r.at<sizeof(T) == 4>(v[e], j + e));
+        *reinterpret_cast<Run<T, N> *>(g + j) = out;
+    } else {
+#pragma unroll
+        for (int e = 0; e < N; ++e)
+            if (j + e < V) store_as(g + j + e, r.at<sizeof(T) == 4>(to_f32(x[j + e]), j + e));
+    }
+}
+
+// Short rows: G lanes to a row, a chunk of N scores each.
+template <typename T, int G, int N>
+__global__ __launch_bounds__(256) void logprobs_grad_short(LogprobGradArgs a)
+{
+    for (int64_t row = (int64_t)blockIdx.x * (256 / G) + threadIdx.x / G; row < a.rows;
+         row += (int64_t)gridDim.x * (256 / G)) {
+        const GradRow r(a, row);
         const T *x = reinterpret_cast<const T *>(a.x) + row * a.stride;
         T *g = reinterpret_cast<T *>(a.g) + row * a.g_stride;
-        float m = a.norm[2 * row], log_s = a.norm[2 * row + 1];
-        const bool empty = m == -INFINITY;
-        const int y = a.labels ? a.labels[row] : -1;
-        float gl = y >= 0 ? a.g_logp[row] : 0.f;
-        if (y >= a.V) m = NAN;
-        const float ge = a.g_entropy ? a.g_entropy[row] : 0.f, ent = a.g_entropy ? a.entropy[row] : 0.f;
-        for (int j = lane; j < a.V; j += 64) {
-            const float lp = (to_f32(x[j]) - m) * a.inv_t - log_s;
-            const float p = expf(lp);
-            float v = gl * ((j == y ? 1.f : 0.f) - p) - ge * p * (fmaxf(lp, -1e30f) + ent);
-            v = empty && y < a.V ? 0.f : v * a.inv_t;
-            store_as(g + j, v);
-        }
+        for (int j = threadIdx.x % G * N; j < a.V; j += G * N) grad_run<T, N>(r, x, g, j, a.V);
     }
 }
 
-int row_grid(int64_t rows, int per_block) { return (int)std::min<int64_t>((rows + per_block - 1) / per_block, 1 << 20); }
+// Long rows: a workgroup to a piece of kU chunks a thread.
+template <typename T>
+__global__ __launch_bounds__(256) void logprobs_grad_long(LogprobGradArgs a, int pieces)
+{
+    constexpr int N = kVec<T>;
+    const int64_t units = a.rows * pieces;
+    for (int64_t unit = blockIdx.x; unit < units; unit += gridDim.x) {
+        const int64_t row = unit / pieces;
+        const int j0 = (int)(unit - row * pieces) * kU * 256 * N;
+        const GradRow r(a, row);
+        const T *x = reinterpret_cast<const T *>(a.x) + row * a.stride;
+        T *g = reinterpret_cast<T *>(a.g) + row * a.g_stride;
+#pragma unroll
+        for (int u = 0; u < kU; ++u) grad_run<T, N>(r, x, g, j0 + (u * 256 + (int)threadIdx.x) * N, a.V);
+    }
+}
+
+int capped(int64_t blocks) { return (int)std::max<int64_t>(1, std::min<int64_t>(blocks, 1 << 22)); }
+
+// -- choices -------------------------------------------------------------------
+constexpr int kShort = 512;  // classes a wave's registers hold at 8 a lane
+
+struct LongPlan {
+    int waves, splits, per_split;
+};
+
+LongPlan long_plan(int64_t rows, int V, int dtype)
+{
+    const int batch = kU * 64 * (dtype == DT_BF16 ? 8 : 4);
+    LongPlan p{V <= 2 * batch ? 1 : 4, 1, V};
+    if (rows <= 512 && V > 8 * batch) {
+        p.waves = 16;
+        // runs of two batches a wave, while there are CUs left to take them
+        const int most = (int)std::min<int64_t>(64, std::max<int64_t>(1, 512 / rows));
+        p.splits = std::min(most, (V + 32 * batch - 1) / (32 * batch));
+        if (p.splits > 1) {
+            p.per_split = ((V + p.splits - 1) / p.splits + 7) / 8 * 8;
+            p.splits = (V + p.per_split - 1) / p.per_split;
+        }
+    }
+    return p;
+}
+
+template <typename T, int G, int C, int N>
+hipError_t go_short(const LogprobArgs &a, hipStream_t s)
+{
+    hipLaunchKernelGGL((logprobs_short<T, G, C, N>), dim3(capped((a.rows + 256 / G - 1) / (256 / G))), dim3(256), 0, s, a);
+    return hipGetLastError();
+}
+
+template <typename T, int W>
+hipError_t go_long(const LogprobArgs &a, const LongPlan &p, char *parts, hipStream_t s)
+{
+    const dim3 grid(capped(a.rows * p.splits)), block(64 * W);
+    const size_t lds = W > 1 ? (size_t)W * a.n_top * 8 : 0;
+    if (a.n_top) hipLaunchKernelGGL((logprobs_long<T, W, true>), grid, block, lds, s, a, p.splits, p.per_split, parts);
+    else hipLaunchKernelGGL((logprobs_long<T, W, false>), grid, block, 0, s, a, p.splits, p.per_split, parts);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess || p.splits == 1) return e;
+    hipLaunchKernelGGL(logprobs_join<T>, dim3(capped(a.rows)), dim3(256), (size_t)p.splits * a.n_top * 8, s, a, p.splits,
+                       (const char *)parts);
+    return hipGetLastError();
+}
+
+template <typename T>
+hipError_t run(const LogprobArgs &a, int dtype, char *parts, hipStream_t s)
+{
+    constexpr int N = kVec<T>, C = 8 / N;  // 8 scores a lane
+    const int V = a.V;
+    if (V <= 2) return go_short<T, 1, 1, 2>(a, s);
+    if (V <= 4) return go_short<T, 1, 1, 4>(a, s);
+    if (V <= 8) return go_short<T, 1, C, N>(a, s);
+    if (V <= 16) return go_short<T, 2, C, N>(a, s);
+    if (V <= 32) return go_short<T, 4, C, N>(a, s);
+    if (V <= 64) return go_short<T, 8, C, N>(a, s);
+    if (V <= 128) return go_short<T, 16, C, N>(a, s);
+    if (V <= 256) return go_short<T, 32, C, N>(a, s);
+    if (V <= kShort) return go_short<T, 64, C, N>(a, s);
+    const LongPlan p = long_plan(a.rows, V, dtype);
+    if (p.waves == 1) return go_long<T, 1>(a, p, parts, s);
+    if (p.waves == 4) return go_long<T, 4>(a, p, parts, s);
+    return go_long<T, 16>(a, p, parts, s);
+}
+
+template <typename T, int G, int N>
+hipError_t go_grad(const LogprobGradArgs &a, hipStream_t s)
+{
+    hipLaunchKernelGGL((logprobs_grad_short<T, G, N>), dim3(capped((a.rows + 256 / G - 1) / (256 / G))), dim3(256), 0, s, a);
+    return hipGetLastError();
+}
+
+template <typename T>
+hipError_t run_grad(const LogprobGradArgs &a, hipStream_t s)
+{
+    constexpr int N = kVec<T>;
+    const int V = a.V;
+    if (V <= 2) return go_grad<T, 1, 2>(a, s);
+    if (V <= 4) return go_grad<T, 1, 4>(a, s);
+    if (V <= 2 * N) return go_grad<T, 2, N>(a, s);
+    if (V <= 4 * N) return go_grad<T, 4, N>(a, s);
+    if (V <= 8 * N) return go_grad<T, 8, N>(a, s);
+    if (V <= 32 * N) return go_grad<T, 16, N>(a, s);
+    if (V <= 256 * N) return go_grad<T, 64, N>(a, s);
+    const int pieces = (V + kU * 256 * N - 1) / (kU * 256 * N);
+    hipLaunchKernelGGL(logprobs_grad_long<T>, dim3(capped(a.rows * pieces)), dim3(256), 0, s, a, pieces);
+    return hipGetLastError();
+}
 
 }  // namespace
 
-size_t logprobs_workspace(int64_t, int, int, int) { return 0; }
-
-hipError_t launch_logprobs(const LogprobArgs &a, int dtype, void *, hipStream_t s)
+size_t logprobs_workspace(int64_t rows, int V, int dtype, int n_top)
 {
-    const dim3 grid(row_grid(a.rows, 4));
-    if (dtype == DT_BF16) hipLaunchKernelGGL(logprobs_row<uint16_t>, grid, dim3(256), 0, s, a);
-    else hipLaunchKernelGGL(logprobs_row<float>, grid, dim3(256), 0, s, a);
-    return hipGetLastError();
+    if (V <= kShort) return 0;
+    const LongPlan p = long_plan(rows, V, dtype);
+    return p.splits > 1 ? (size_t)rows * p.splits * split_bytes(n_top) : 0;
+}
+
+hipError_t launch_logprobs(const LogprobArgs &a, int dtype, void *ws, hipStream_t s)
+{
+    return dtype == DT_BF16 ? run<uint16_t>(a, dtype, (char *)ws, s) : run<float>(a, dtype, (char *)ws, s);
 }
 
 hipError_t launch_logprobs_grad(const LogprobGradArgs &a, int dtype, hipStream_t s)
 {
-    const dim3 grid(row_grid(a.rows, 4));
-    if (dtype == DT_BF16) hipLaunchKernelGGL(logprobs_grad_row<uint16_t>, grid, dim3(256), 0, s, a);
-    else hipLaunchKernelGGL(logprobs_grad_row<float>, grid, dim3(256), 0, s, a);
-    return hipGetLastError();
+    return dtype == DT_BF16 ? run_grad<uint16_t>(a, s) : run_grad<float>(a, s);
 }
 
 }  // namespace fs
