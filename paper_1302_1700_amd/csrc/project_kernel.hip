@@ -1,154 +1,546 @@
 // A fully connected layer on rows with a low-rank adapter of each row's own
 // choice, and its gradient:  y = W x + bias + s_i B_i (A_i x), i = ids[row].
-// One thread per output value, one wave per row's product with a factor.
+//
+// Few outputs (m + rank up to 64): one pass over the rows, in which the rows
+// of W and of A_i are the columns of one product (project_narrow); more: the
+// rows times A_i first (rank_rows), then a tiled product that adds B_i's part
+// (project_wide.hip).  The factors' gradients: per adapter, sums over its rows
+// of outer products, in runs of rows joined by a second launch in the order of
+// the runs (factor_grad, factor_join).
 #include <algorithm>
 
-#include "rows.h"
+#include "project.h"
 
 namespace fs {
 namespace {
 
-__device__ __forceinline__ float wave_sum(float v)
+// Rows [16 RB] of a wave times `cols` columns, column c from src(c) (null: 0),
+// summed over [c0, c1) of the shared axis.
+template <bool GATHER, typename T, int RB, int NB>
+__device__ __forceinline__ void row_products(const T *const (&row)[RB], const T *const (&col)[NB], int64_t col_step,
+                                             int c0, int c1, f4 (&acc)[RB][NB])
 {
+    constexpr int E = Operand<T>::kE, U = NB == 1 ? 4 : 2;  // steps whose loads are in flight together
+    const int g = (threadIdx.x & 63) >> 4;
+    auto load = [&](int c, int have, Operand<T>(&oa)[RB], Operand<T>(&ob)[NB]) {
 #pragma unroll
-    for (int d = 32; d; d >>= 1) v += __shfl_xor(v, d);
-    return v;
+        for (int i = 0; i < RB; ++i) oa[i] = load_operand(row[i] + c, have);
+#pragma unroll
+        for (int j = 0; j < NB; ++j) {
+            ob[j] = Operand<T>{};
+            if (col[j]) ob[j] = GATHER ? gather_operand(col[j] + c * col_step, col_step, have) : load_operand(col[j] + c, have);
+        }
+    };
+    auto multiply = [&](const Operand<T>(&oa)[RB], const Operand<T>(&ob)[NB]) {
+#pragma unroll
+        for (int i = 0; i < RB; ++i)
+#pragma unroll
+            for (int j = 0; j < NB; ++j) acc[i][j] = block_product(oa[i], ob[j], acc[i][j]);
+    };
+    int c = c0 + g * E, at = c0;
+    for (; at + U * kStep<T> <= c1; at += U * kStep<T>, c += U * kStep<T>) {
+        Operand<T> oa[U][RB], ob[U][NB];
+#pragma unroll
+        for (int u = 0; u < U; ++u) load(c + u * kStep<T>, E, oa[u], ob[u]);
+#pragma unroll
+        for (int u = 0; u < U; ++u) multiply(oa[u], ob[u]);
+    }
+    for (; at < c1; at += kStep<T>, c += kStep<T>) {
+        Operand<T> oa[RB], ob[NB];
+        load(c, c1 - c, oa, ob);
+        multiply(oa, ob);
+    }
 }
 
-// out[row][j] = s * sum_c v[row][c] f[i][...]: f [n][r][C] (by_rank) or [n][C][r]
-template <typename T>
-__global__ __launch_bounds__(256) void factor_rows(const T *v, int64_t vs, int64_t rows, int C, const T *f, int by_rank,
-                                                   int n, int r, const float *scale, const int *ids, float *out)
+// Rows times a factor, t[row][j] = s_i sum_c v[row][c] f_i[j][c]: f [n][r][C]
+// (TRANS false: A) or [n][C][r] (true: B).  A wave takes 16 rows, W waves share
+// the summed axis of them.
+template <typename T, int NB, int W, bool TRANS>
+__global__ __launch_bounds__(256) void rank_rows(const T *v, int64_t vs, int64_t rows, int C, const T *f, int n, int r,
+                                                 const float *scale, const int *ids, float *t)
 {
-    const int lane = threadIdx.x & 63;
-    for (int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); row < rows; row += (int64_t)gridDim.x * 4) {
-        const int i = ids[row];
-        for (int j = 0; j < r; ++j) {
-            float t = 0.f;
-            if (i >= 0 && i < n) {
-                const T *fi = f + (int64_t)i * r * C;
-                for (int c = lane; c < C; c += 64)
-                    t = fmaf(to_f32(v[row * vs + c]), to_f32(by_rank ? fi[(int64_t)j * C + c] : fi[(int64_t)c * r + j]), t);
-                t = wave_sum(t);
-                if (scale) t *= scale[i];
+    __shared__ float part[W > 1 ? 4 * 16 * NB * 16 : 1];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, q = lane & 15, g = lane >> 4;
+    const int64_t tiles = (rows + 15) / 16;
+    constexpr int PER = 4 / W;  // tiles of a workgroup
+    for (int64_t tile0 = (int64_t)blockIdx.x * PER; tile0 < tiles; tile0 += (int64_t)gridDim.x * PER) {
+        const int64_t row0 = (tile0 + wave / W) * 16;
+        const int id = row0 + q < rows ? ids[row0 + q] : -1;
+        const T *row[1] = {v + clamp_row(row0 + q, rows) * vs};
+        constexpr int S = kStep<T>;
+        const int run = W == 1 ? C : (C + W * S - 1) / (W * S) * S;
+        const int c0 = std::min(C, wave % W * run), c1 = std::min(C, c0 + run);
+        float out[NB][4];
+#pragma unroll
+        for (int j = 0; j < NB; ++j)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) out[j][e] = 0.f;
+        for (int last = -1;;) {
+            const int cur = next_adapter(id, last);
+            if (cur >= n) break;
+            last = cur;
+            const T *col[NB];
+            f4 acc[1][NB];
+#pragma unroll
+            for (int j = 0; j < NB; ++j) {
+                const int c = j * 16 + q;
+                col[j] = c >= r ? nullptr : TRANS ? f + (int64_t)cur * r * C + c : f + ((int64_t)cur * r + c) * C;
+                acc[0][j] = f4{0.f, 0.f, 0.f, 0.f};
             }
-            if (lane == 0) out[row * r + j] = i >= n ? NAN : t;
+            row_products<TRANS, T, 1, NB>(row, col, r, c0, c1, acc);
+            if constexpr (W > 1) {
+                __syncthreads();
+#pragma unroll
+                for (int j = 0; j < NB; ++j)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) part[((wave * NB + j) * 4 + e) * 64 + lane] = acc[0][j][e];
+                __syncthreads();
+#pragma unroll
+                for (int j = 0; j < NB; ++j)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        float s = 0.f;
+#pragma unroll
+                        for (int k = 0; k < W; ++k) s += part[((k * NB + j) * 4 + e) * 64 + lane];
+                        acc[0][j][e] = s;
+                    }
+            }
+            const float sc = scale ? scale[cur] : 1.f;
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (__shfl(id, g * 4 + e) == cur) {
+#pragma unroll
+                    for (int j = 0; j < NB; ++j) out[j][e] = acc[0][j][e] * sc;
+                }
+        }
+        if (wave % W == 0) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int64_t to = row0 + g * 4 + e;
+                const bool bad = __shfl(id, g * 4 + e) >= n;
+#pragma unroll
+                for (int j = 0; j < NB; ++j)
+                    if (to < rows && j * 16 + q < r) t[to * r + j * 16 + q] = bad ? NAN : out[j][e];
+            }
         }
     }
 }
 
-template <typename T>
-__global__ __launch_bounds__(256) void project_each(ProjArgs a, T *y, int64_t ys, const float *h)
+// Few outputs: columns 0 .. M - 1 of the product are W's rows, the next r
+// A_i's; the products go through LDS, where each row's outputs take up their
+// hidden values.  A wave takes 16 RB rows (W = 1), or 16 shared by W waves.
+template <typename T, int RB, int NB, int W>
+__global__ __launch_bounds__(256) void project_narrow(ProjArgs a, T *y, int64_t ys, float *hidden)
 {
-    const T *x = (const T *)a.x, *w = (const T *)a.w, *b = (const T *)a.b;
-    const int64_t total = a.rows * a.M;
-    for (int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x; t < total; t += (int64_t)gridDim.x * 256) {
-        const int64_t row = t / a.M;
-        const int m = (int)(t - row * a.M);
-        float v = 0.f;
-        for (int c = 0; c < a.K; ++c) v = fmaf(to_f32(x[row * a.xs + c]), to_f32(w[m * a.ws + c]), v);
-        const int i = a.n ? a.ids[row] : -1;
-        if (i >= a.n) v = NAN;
-        else if (i >= 0) {
-            float z = 0.f;
-            for (int j = 0; j < a.r; ++j) z = fmaf(h[row * a.r + j], to_f32(b[((int64_t)i * a.M + m) * a.r + j]), z);
-            v += a.scale ? z * a.scale[i] : z;
+    constexpr int P = NB * 16 + 1;
+    __shared__ float part[4][16 * RB][P];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, q = lane & 15, g = lane >> 4;
+    const int64_t tiles = (a.rows + 16 * RB - 1) / (16 * RB);
+    constexpr int PER = 4 / W;
+    const T *x = (const T *)a.x, *w = (const T *)a.w, *fa = (const T *)a.a, *fb = (const T *)a.b;
+    const int M = a.M, r = a.r, n = a.n;
+    for (int64_t tile0 = (int64_t)blockIdx.x * PER; tile0 < tiles; tile0 += (int64_t)gridDim.x * PER) {
+        const int64_t row0 = (tile0 + wave / W) * 16 * RB;
+        int id = -1;  // of row `lane` of the wave's; a bad one stands as "none" in the walk
+        if (n && lane < 16 * RB && row0 + lane < a.rows) id = a.ids[row0 + lane];
+        const bool bad = id >= n;
+        int group = lane < 16 * RB && row0 + lane < a.rows ? (bad || id < 0 ? 0 : id + 1) : -1;
+        const T *row[RB];
+#pragma unroll
+        for (int i = 0; i < RB; ++i) row[i] = x + clamp_row(row0 + i * 16 + q, a.rows) * a.xs;
+        constexpr int S = kStep<T>;
+        const int run = W == 1 ? a.K : (a.K + W * S - 1) / (W * S) * S;
+        const int c0 = std::min(a.K, wave % W * run), c1 = std::min(a.K, c0 + run);
+        for (int last = -1;;) {
+            const int cur = next_adapter(group, last);  // 0: rows without an adapter, i + 1: adapter i
+            if (cur > n) break;
+            last = cur;
+            const T *ai = cur ? fa + (int64_t)(cur - 1) * r * a.K : nullptr;
+            const T *col[NB];
+            f4 acc[RB][NB];
+#pragma unroll
+            for (int j = 0; j < NB; ++j) {
+                const int c = j * 16 + q;
+                col[j] = c < M ? w + c * a.ws : ai && c < M + r ? ai + (int64_t)(c - M) * a.K : nullptr;
+#pragma unroll
+                for (int i = 0; i < RB; ++i) acc[i][j] = f4{0.f, 0.f, 0.f, 0.f};
+            }
+            row_products<false, T, RB, NB>(row, col, 1, c0, c1, acc);
+            if (W > 1) __syncthreads();
+#pragma unroll
+            for (int i = 0; i < RB; ++i)
+#pragma unroll
+                for (int j = 0; j < NB; ++j)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) part[wave][i * 16 + g * 4 + e][j * 16 + q] = acc[i][j][e];
+            if (W > 1) {
+                __syncthreads();
+                for (int k = threadIdx.x; k < 16 * RB * (M + r); k += 256) {
+                    const int rr = k / (M + r), c = k - rr * (M + r);
+                    float s = part[0][rr][c];
+#pragma unroll
+                    for (int o = 1; o < W; ++o) s += part[o][rr][c];
+                    part[0][rr][c] = s;
+                }
+                __syncthreads();
+            } else {
+                __builtin_amdgcn_wave_barrier();
+            }
+            const float(*sum)[P] = part[W > 1 ? 0 : wave];
+            const float sc = cur && a.scale ? a.scale[cur - 1] : 1.f;
+            if (wave % W == 0) {
+                for (int k = lane; k < (16 * RB * M + 63) / 64 * 64; k += 64) {
+                    const int rr = k / M, m = k - rr * M;
+                    const bool mine = __shfl(group, rr & 63) == cur && rr < 16 * RB;
+                    const bool none = __shfl((int)bad, rr & 63);
+                    if (!mine) continue;
+                    float v = sum[rr][m];
+                    if (cur) {
+                        const T *bi = fb + ((int64_t)(cur - 1) * M + m) * r;
+                        float z = 0.f;
+                        for (int j = 0; j < r; ++j) z = fmaf(sum[rr][M + j], to_f32(bi[j]), z);
+                        v = fmaf(z, sc, v);
+                    }
+                    if (a.bias) v += a.bias[m];
+                    store_as(y + (row0 + rr) * ys + m, none ? NAN : v);
+                }
+                if (hidden) {
+                    for (int k = lane; k < (16 * RB * r + 63) / 64 * 64; k += 64) {
+                        const int rr = k / r, j = k - rr * r;
+                        const bool mine = __shfl(group, rr & 63) == cur && rr < 16 * RB;
+                        const bool none = __shfl((int)bad, rr & 63);
+                        if (mine) hidden[(row0 + rr) * r + j] = none ? NAN : cur ? sum[rr][M + j] : 0.f;
+                    }
+                }
+            }
+            if (W == 1) __builtin_amdgcn_wave_barrier();
         }
-        store_as(y + row * ys + m, a.bias ? v + a.bias[m] : v);
+        if (W > 1) __syncthreads();
     }
 }
 
+// One of the two factors' gradients: out_i[j][c] = s_i? sum over rows of i of
+// t[row][j] v[row][c], stored [n][r][C] (by_rank) or [n][C][r].
 template <typename T>
-__global__ __launch_bounds__(256) void grad_rows_each(ProjArgs a, const T *g, int64_t gs, const float *u, T *gx, int64_t gxs)
+struct FactorJob {
+    const float *t;
+    const T *v;
+    int64_t vs;
+    int C, by_rank, ctiles;
+    const float *scale;
+    T *out;
+    float *parts;  // [n][runs][r][C]
+};
+
+template <typename T>
+struct FactorArgs {
+    FactorJob<T> job[2];
+    int64_t rows;
+    int run_rows, runs, n, r;
+    const int *ids;
+    uint8_t *used;  // [n][runs]: the run holds rows of the adapter
+};
+
+// Columns of a workgroup: 64 KB' worth of accumulators, 16 ranks a block.
+template <int NB>
+constexpr int kFactorCols = NB == 1 ? 256 : NB == 2 ? 128 : 64;
+
+// Workgroup: one adapter, one run of rows, one tile of columns.  The run's rows
+// that name the adapter are listed in LDS, 1024 ids at a time; the four waves
+// take four listed rows each in turn as the summed axis of float32 products
+// (bf16 values are exact in them).
+template <typename T, int NB>
+__global__ __launch_bounds__(256) void factor_grad(FactorArgs<T> a)
 {
-    const T *w = (const T *)a.w, *fa = (const T *)a.a;
-    const int64_t total = a.rows * a.K;
-    for (int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x; t < total; t += (int64_t)gridDim.x * 256) {
-        const int64_t row = t / a.K;
-        const int k = (int)(t - row * a.K);
-        float v = 0.f;
-        for (int m = 0; m < a.M; ++m) v = fmaf(to_f32(g[row * gs + m]), to_f32(w[m * a.ws + k]), v);
-        const int i = a.n ? a.ids[row] : -1;
-        if (i >= a.n) v = NAN;
-        else if (i >= 0)
-            for (int j = 0; j < a.r; ++j) v = fmaf(u[row * a.r + j], to_f32(fa[((int64_t)i * a.r + j) * a.K + k]), v);
-        store_as(gx + row * gxs + k, v);
+    constexpr int CT = kFactorCols<NB>, CB = CT / 64;
+    __shared__ int list[1024 + 16];
+    __shared__ int count[17];
+    __shared__ float sums[4][64][NB * 4 + 1];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, q = lane & 15, g = lane >> 4;
+    const int which = blockIdx.x >= (unsigned)a.job[0].ctiles;
+    const FactorJob<T> &job = a.job[which];
+    const int c0 = ((int)blockIdx.x - (which ? a.job[0].ctiles : 0)) * CT;
+    const int r = a.r;
+    for (int64_t unit = blockIdx.y; unit < (int64_t)a.n * a.runs; unit += gridDim.y) {
+        const int i = (int)(unit / a.runs), run = (int)(unit - (int64_t)i * a.runs);
+        const int64_t begin = (int64_t)run * a.run_rows, end = std::min(a.rows, begin + a.run_rows);
+        f4 acc[CB * 4][NB];
+#pragma unroll
+        for (int b = 0; b < CB * 4; ++b)
+#pragma unroll
+            for (int j = 0; j < NB; ++j) acc[b][j] = f4{0.f, 0.f, 0.f, 0.f};
+        bool seen = false;
+        for (int64_t at = begin; at < end; at += 1024) {
+            // the listed rows, in their order: sixteen groups of 64 ids
+            __syncthreads();
+            uint64_t who[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const int64_t row = at + (wave * 4 + k) * 64 + lane;
+                who[k] = __ballot(row < end && a.ids[std::min(row, a.rows - 1)] == i);
+                if (lane == 0) count[wave * 4 + k] = __popcll(who[k]);
+            }
+            __syncthreads();
+            int total = 0, before = 0;
+#pragma unroll
+            for (int k = 0; k < 16; ++k) {
+                if (k < wave * 4) before += count[k];
+                total += count[k];
+            }
+            if (total == 0) continue;
+            seen = true;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const int below = __popcll(who[k] & ((1ull << lane) - 1));
+                if (who[k] >> lane & 1) list[before + below] = (wave * 4 + k) * 64 + lane;
+                before += __popcll(who[k]);
+            }
+            __syncthreads();
+            for (int l = wave * 4; l < total; l += 16) {
+                const bool have = l + g < total;
+                const int64_t row = at + list[have ? l + g : l];
+                float tv[NB];
+#pragma unroll
+                for (int j = 0; j < NB; ++j) tv[j] = have && j * 16 + q < r ? job.t[row * r + j * 16 + q] : 0.f;
+                const T *v = job.v + row * job.vs;
+#pragma unroll
+                for (int b = 0; b < CB; ++b) {
+                    const int c = c0 + b * 64 + q * 4;
+                    float vv[4];
+                    if (c + 4 <= job.C) {
+                        struct __attribute__((packed, aligned(alignof(T)))) Quad { T v[4]; };
+                        const Quad w = *reinterpret_cast<const Quad *>(v + c);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) vv[e] = to_f32(w.v[e]);
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) vv[e] = c + e < job.C ? to_f32(v[c + e]) : 0.f;
+                    }
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const float ve = have ? vv[e] : 0.f;
+#pragma unroll
+                        for (int j = 0; j < NB; ++j)
+                            acc[b * 4 + e][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(tv[j], ve, acc[b * 4 + e][j], 0, 0, 0);
+                    }
+                }
+            }
+        }
+        if (threadIdx.x == 0 && blockIdx.x == 0 && a.used) a.used[unit] = seen;
+        if (!seen && a.runs > 1) continue;
+        // the waves' sums joined block by block; ranks 16 j + 4 g + e, column 64 b + 4 q + p
+        const float sc = job.scale ? job.scale[i] : 1.f;
+#pragma unroll
+        for (int bp = 0; bp < CB * 4; ++bp) {
+            __syncthreads();
+#pragma unroll
+            for (int j = 0; j < NB; ++j)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) sums[wave][lane][j * 4 + e] = acc[bp][j][e];
+            __syncthreads();
+            for (int k = threadIdx.x; k < 64 * NB * 4; k += 256) {
+                const int l = k & 63, je = k >> 6;
+                const float s = sums[0][l][je] + sums[1][l][je] + sums[2][l][je] + sums[3][l][je];
+                const int j = je / 4 * 16 + (l >> 4) * 4 + je % 4, c = c0 + (bp >> 2) * 64 + (l & 15) * 4 + (bp & 3);
+                if (j >= r || c >= job.C) continue;
+                if (a.runs > 1) job.parts[((unit * r) + j) * job.C + c] = s;
+                else {
+                    const int64_t o = job.by_rank ? ((int64_t)i * r + j) * job.C + c : ((int64_t)i * job.C + c) * r + j;
+                    store_as(job.out + o, s * sc);
+                }
+            }
+        }
     }
 }
 
-// out[i][j][c] (or [i][c][j]) = sum over rows of adapter i of s_i? * t[row][j] v[row][c]
+// Sums the runs' parts in the order of the runs.
 template <typename T>
-__global__ __launch_bounds__(256) void factor_grad_each(const float *t, const T *v, int64_t vs, int64_t rows, int C, int n,
-                                                        int r, const float *scale, const int *ids, T *out, int by_rank)
+__global__ __launch_bounds__(256) void factor_join(FactorArgs<T> a)
 {
-    const int64_t total = (int64_t)n * r * C;
-    for (int64_t q = (int64_t)blockIdx.x * 256 + threadIdx.x; q < total; q += (int64_t)gridDim.x * 256) {
-        const int c = (int)(q % C), j = (int)(q / C % r), i = (int)(q / C / r);
-        double s = 0;
-        for (int64_t row = 0; row < rows; ++row)
-            if (ids[row] == i) s += (double)(t[row * r + j] * to_f32(v[row * vs + c]));
-        if (scale) s *= scale[i];
-        store_as(out + (by_rank ? q : ((int64_t)i * C + c) * r + j), (float)s);
+    const FactorJob<T> &job = a.job[blockIdx.y];
+    const int64_t total = (int64_t)a.n * a.r * job.C;
+    for (int64_t k = (int64_t)blockIdx.x * 256 + threadIdx.x; k < total; k += (int64_t)gridDim.x * 256) {
+        const int c = (int)(k % job.C), j = (int)(k / job.C % a.r), i = (int)(k / job.C / a.r);
+        float s = 0.f;
+        for (int run = 0; run < a.runs; ++run) {
+            const int64_t unit = (int64_t)i * a.runs + run;
+            if (a.used[unit]) s += job.parts[(unit * a.r + j) * job.C + c];
+        }
+        if (job.scale) s *= job.scale[i];
+        store_as(job.out + (job.by_rank ? k : ((int64_t)i * job.C + c) * a.r + j), s);
     }
 }
 
-int grid_for(int64_t n, int per) { return (int)std::max<int64_t>(1, std::min<int64_t>((n + per - 1) / per, 1 << 20)); }
+// -- choices and workspace ---------------------------------------------------------
+size_t up256(size_t v) { return (v + 255) & ~(size_t)255; }
+size_t rank_bytes(const ProjArgs &a) { return up256((size_t)a.rows * a.r * sizeof(float)); }
+bool narrow(const ProjArgs &a) { return a.M + a.r <= 64; }
 
-size_t rank_rows(const ProjArgs &a) { return ((size_t)a.rows * a.r * sizeof(float) + 255) & ~(size_t)255; }
-
+// Four waves share the summed axis while whole waves to a tile of rows would
+// leave CUs idle.  The same rule wherever rows meet A: the hidden rows then
+// have the same bits from every kernel.
 template <typename T>
-hipError_t project(const ProjArgs &a, T *y, int64_t ys, float *h, hipStream_t s)
+bool share_axis(int64_t rows, int C) { return rows <= 16 * 4096 && C >= 8 * kStep<T>; }
+
+struct RunPlan {
+    int run_rows, runs;
+    size_t parts[2], used;  // bytes
+};
+
+// Runs of rows: enough workgroups for the card where the rows of an adapter lie
+// together (then one in n of them works), parts of at most 256 MB.
+RunPlan run_plan(const ProjArgs &a)
 {
-    if (a.n)
-        hipLaunchKernelGGL(factor_rows<T>, dim3(grid_for(a.rows, 4)), dim3(256), 0, s, (const T *)a.x, a.xs, a.rows, a.K,
-                           (const T *)a.a, 1, a.n, a.r, nullptr, a.ids, h);
-    hipLaunchKernelGGL(project_each<T>, dim3(grid_for(a.rows * a.M, 256)), dim3(256), 0, s, a, y, ys, h);
+    const int nb = a.r <= 16 ? 1 : a.r <= 32 ? 2 : 4, ct = nb == 1 ? 256 : nb == 2 ? 128 : 64;
+    const int64_t ctiles = (a.K + ct - 1) / ct + (a.M + ct - 1) / ct;
+    const double part = (double)a.n * a.r * (a.K + a.M) * sizeof(float);
+    int64_t runs = std::max<int64_t>(1, std::min<int64_t>(1024 / ctiles, a.rows / 512));
+    runs = std::max<int64_t>(1, std::min<int64_t>(runs, (int64_t)(268435456.0 / part)));
+    RunPlan p;
+    p.run_rows = (int)(((a.rows + runs - 1) / runs + 63) / 64 * 64);
+    p.run_rows = std::max(p.run_rows, 64);
+    p.runs = (int)std::max<int64_t>(1, (a.rows + p.run_rows - 1) / p.run_rows);
+    p.parts[0] = p.runs > 1 ? up256((size_t)a.n * p.runs * a.r * a.K * sizeof(float)) : 0;
+    p.parts[1] = p.runs > 1 ? up256((size_t)a.n * p.runs * a.r * a.M * sizeof(float)) : 0;
+    p.used = p.runs > 1 ? up256((size_t)a.n * p.runs) : 0;
+    return p;
+}
+
+template <typename T, int NB, bool TRANS>
+hipError_t go_rank(const T *v, int64_t vs, int64_t rows, int C, const T *f, int n, int r, const float *scale,
+                   const int *ids, float *t, hipStream_t s)
+{
+    const int64_t tiles = (rows + 15) / 16;
+    if (share_axis<T>(rows, C))
+        hipLaunchKernelGGL((rank_rows<T, NB, 4, TRANS>), dim3(grid_of(tiles)), dim3(256), 0, s, v, vs, rows, C, f, n, r,
+                           scale, ids, t);
+    else
+        hipLaunchKernelGGL((rank_rows<T, NB, 1, TRANS>), dim3(grid_of((tiles + 3) / 4)), dim3(256), 0, s, v, vs, rows, C,
+                           f, n, r, scale, ids, t);
+    return hipGetLastError();
+}
+
+template <typename T, bool TRANS>
+hipError_t rank_product(const T *v, int64_t vs, int64_t rows, int C, const T *f, int n, int r, const float *scale,
+                        const int *ids, float *t, hipStream_t s)
+{
+    if (r <= 16) return go_rank<T, 1, TRANS>(v, vs, rows, C, f, n, r, scale, ids, t, s);
+    if (r <= 32) return go_rank<T, 2, TRANS>(v, vs, rows, C, f, n, r, scale, ids, t, s);
+    if (r <= 64) return go_rank<T, 4, TRANS>(v, vs, rows, C, f, n, r, scale, ids, t, s);
+    return go_rank<T, 8, TRANS>(v, vs, rows, C, f, n, r, scale, ids, t, s);
+}
+
+template <typename T, int NB>
+hipError_t go_narrow(const ProjArgs &a, T *y, int64_t ys, float *hidden, hipStream_t s)
+{
+    const int64_t tiles = (a.rows + 15) / 16;
+    if (share_axis<T>(a.rows, a.K)) {
+        hipLaunchKernelGGL((project_narrow<T, 1, NB, 4>), dim3(grid_of(tiles)), dim3(256), 0, s, a, y, ys, hidden);
+    } else {
+        constexpr int RB = 2;
+        hipLaunchKernelGGL((project_narrow<T, RB, NB, 1>), dim3(grid_of((tiles + 4 * RB - 1) / (4 * RB))), dim3(256), 0, s,
+                           a, y, ys, hidden);
+    }
     return hipGetLastError();
 }
 
 template <typename T>
-hipError_t project_grad(const ProjArgs &a, const T *g, int64_t gs, const float *h, T *gx, int64_t gxs, T *ga, T *gb,
-                        float *hw, float *u, hipStream_t s)
+hipError_t project(const ProjArgs &a, int dtype, T *y, int64_t ys, float *hidden, float *h, hipStream_t s)
 {
+    if (narrow(a)) {
+        const int cols = a.M + a.r;
+        if (cols <= 16) return go_narrow<T, 1>(a, y, ys, hidden, s);
+        if (cols <= 32) return go_narrow<T, 2>(a, y, ys, hidden, s);
+        return go_narrow<T, 4>(a, y, ys, hidden, s);
+    }
+    if (a.n) {
+        hipError_t e = rank_product<T, false>((const T *)a.x, a.xs, a.rows, a.K, (const T *)a.a, a.n, a.r, nullptr, a.ids, h, s);
+        if (e != hipSuccess) return e;
+    }
+    const WideArgs w{a.x, a.w, a.b, y, a.rows, a.xs, a.ws, ys, a.K, a.M, a.n, a.r, a.bias, a.scale, h, a.ids};
+    return launch_wide(w, dtype, false, s);
+}
+
+template <typename T, int NB>
+hipError_t go_factor(const FactorArgs<T> &a, hipStream_t s)
+{
+    const int64_t units = (int64_t)a.n * a.runs;
+    hipLaunchKernelGGL((factor_grad<T, NB>), dim3(a.job[0].ctiles + a.job[1].ctiles, (unsigned)std::min<int64_t>(units, 65535)),
+                       dim3(256), 0, s, a);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess || a.runs == 1) return e;
+    const int64_t most = (int64_t)a.n * a.r * std::max(a.job[0].C, a.job[1].C);
+    hipLaunchKernelGGL(factor_join<T>, dim3(grid_of((most + 255) / 256), 2), dim3(256), 0, s, a);
+    return hipGetLastError();
+}
+
+template <typename T>
+hipError_t project_grad(const ProjArgs &a, int dtype, const T *g, int64_t gs, const float *h, T *gx, int64_t gxs, T *ga,
+                        T *gb, char *ws, hipStream_t s)
+{
+    hipError_t e;
+    float *u = (float *)ws;
+    ws += rank_bytes(a);
+    float *own = (float *)ws;
+    ws += rank_bytes(a);
     if (a.n && a.rows) {
-        hipLaunchKernelGGL(factor_rows<T>, dim3(grid_for(a.rows, 4)), dim3(256), 0, s, g, gs, a.rows, a.M, (const T *)a.b,
-                           0, a.n, a.r, a.scale, a.ids, u);
+        e = rank_product<T, true>(g, gs, a.rows, a.M, (const T *)a.b, a.n, a.r, a.scale, a.ids, u, s);
+        if (e != hipSuccess) return e;
         if (!h && ga) {
-            hipLaunchKernelGGL(factor_rows<T>, dim3(grid_for(a.rows, 4)), dim3(256), 0, s, (const T *)a.x, a.xs, a.rows,
-                               a.K, (const T *)a.a, 1, a.n, a.r, nullptr, a.ids, hw);
-            h = hw;
+            e = rank_product<T, false>((const T *)a.x, a.xs, a.rows, a.K, (const T *)a.a, a.n, a.r, nullptr, a.ids, own, s);
+            if (e != hipSuccess) return e;
+            h = own;
         }
     }
-    if (gx && a.rows)
-        hipLaunchKernelGGL(grad_rows_each<T>, dim3(grid_for(a.rows * a.K, 256)), dim3(256), 0, s, a, g, gs, u, gx, gxs);
     if (ga) {
-        hipLaunchKernelGGL(factor_grad_each<T>, dim3(grid_for((int64_t)a.n * a.r * a.K, 256)), dim3(256), 0, s, u,
-                           (const T *)a.x, a.xs, a.rows, a.K, a.n, a.r, nullptr, a.ids, ga, 1);
-        hipLaunchKernelGGL(factor_grad_each<T>, dim3(grid_for((int64_t)a.n * a.r * a.M, 256)), dim3(256), 0, s, h, g, gs,
-                           a.rows, a.M, a.n, a.r, a.scale, a.ids, gb, 0);
+        const RunPlan p = run_plan(a);
+        const int nb = a.r <= 16 ? 1 : a.r <= 32 ? 2 : a.r <= 64 ? 4 : 8;
+        const int ct = nb == 1 ? 256 : nb == 2 ? 128 : 64;
+        FactorArgs<T> f{};
+        f.job[0] = FactorJob<T>{u, (const T *)a.x, a.xs, a.K, 1, (a.K + ct - 1) / ct, nullptr, ga, (float *)ws};
+        f.job[1] = FactorJob<T>{h, g, gs, a.M, 0, (a.M + ct - 1) / ct, a.scale, gb, (float *)(ws + p.parts[0])};
+        f.rows = a.rows;
+        f.run_rows = p.run_rows;
+        f.runs = p.runs;
+        f.n = a.n;
+        f.r = a.r;
+        f.ids = a.ids;
+        f.used = p.runs > 1 ? (uint8_t *)(ws + p.parts[0] + p.parts[1]) : nullptr;
+        e = nb == 1 ? go_factor<T, 1>(f, s) : nb == 2 ? go_factor<T, 2>(f, s) : nb == 4 ? go_factor<T, 4>(f, s)
+                                                                                        : go_factor<T, 8>(f, s);
+        if (e != hipSuccess) return e;
     }
-    return hipGetLastError();
+    if (gx && a.rows) {
+        const WideArgs w{g, a.w, a.a, gx, a.rows, gs, a.ws, gxs, a.M, a.K, a.n, a.r, nullptr, nullptr, u, a.ids};
+        return launch_wide(w, dtype, true, s);
+    }
+    return hipSuccess;
 }
 
 }  // namespace
 
-size_t project_workspace(const ProjArgs &a, int) { return rank_rows(a); }
+size_t project_workspace(const ProjArgs &a, int) { return narrow(a) ? 0 : rank_bytes(a); }
 
 hipError_t launch_project(const ProjArgs &a, int dtype, void *y, int64_t ys, float *hidden, void *ws, hipStream_t s)
 {
     float *h = hidden ? hidden : (float *)ws;
-    return dtype == DT_BF16 ? project(a, (uint16_t *)y, ys, h, s) : project(a, (float *)y, ys, h, s);
+    return dtype == DT_BF16 ? project(a, dtype, (uint16_t *)y, ys, hidden, h, s) : project(a, dtype, (float *)y, ys, hidden, h, s);
 }
 
-size_t project_grad_workspace(const ProjArgs &a, int) { return 2 * rank_rows(a); }
+size_t project_grad_workspace(const ProjArgs &a, int)
+{
+    if (!a.n) return 0;
+    const RunPlan p = run_plan(a);
+    return 2 * rank_bytes(a) + p.parts[0] + p.parts[1] + p.used;
+}
 
 hipError_t launch_project_grad(const ProjArgs &a, int dtype, const void *g, int64_t gs, const float *hidden, void *gx,
                                int64_t gxs, void *ga, void *gb, void *ws, hipStream_t s)
 {
-    float *u = (float *)ws, *hw = (float *)((char *)ws + rank_rows(a));
     if (dtype == DT_BF16)
-        return project_grad(a, (const uint16_t *)g, gs, hidden, (uint16_t *)gx, gxs, (uint16_t *)ga, (uint16_t *)gb, hw, u, s);
-    return project_grad(a, (const float *)g, gs, hidden, (float *)gx, gxs, (float *)ga, (float *)gb, hw, u, s);
+        return project_grad(a, dtype, (const uint16_t *)g, gs, hidden, (uint16_t *)gx, gxs, (uint16_t *)ga, (uint16_t *)gb,
+                            (char *)ws, s);
+    return project_grad(a, dtype, (const float *)g, gs, hidden, (float *)gx, gxs, (float *)ga, (float *)gb, (char *)ws, s);
 }
 
 }  // namespace fs
