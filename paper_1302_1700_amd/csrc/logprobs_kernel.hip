@@ -22,22 +22,14 @@ constexpr float kLowest = -3.402823466e38f;
 constexpr float kLog2e = 1.44269504088896f, kLn2 = 0.693147180559945f;
 constexpr float kFar = -1e30f;
 
-// Elements per 16-byte load, and the load itself: rows start anywhere their
-// element type may, and the memory pipeline takes such addresses.
+// Elements per 16-byte load: rows start anywhere their element type may.
 template <typename T>
 constexpr int kVec = 16 / sizeof(T);
 
 template <typename T, int N>
-struct __attribute__((packed, aligned(alignof(T)))) Run {
-    T v[N];
-};
-
-template <typename T, int N>
 __device__ __forceinline__ void load_run(const T *p, float *v)
 {
-    const Run<T, N> r = *reinterpret_cast<const Run<T, N> *>(p);
-#pragma unroll
-    for (int e = 0; e < N; ++e) v[e] = to_f32(r.v[e]);
+    unpack<T, N>(load_words<N * sizeof(T)>(p), v);
 }
 
 // Scores in the order of their values, equal ones by their class: the float as
@@ -124,7 +116,10 @@ __device__ __forceinline__ float label_logp(const RowStats &r, int y, int V, flo
 
 __device__ __forceinline__ void store_stats(const LogprobArgs &a, int64_t row, const RowStats &r, int y, float xy)
 {
-    if (a.norm) *reinterpret_cast<Run<float, 2> *>(a.norm + 2 * row) = Run<float, 2>{{r.m, r.log_s}};
+    if (a.norm) {
+        const float v[2] = {r.m, r.log_s};
+        store_words<8>(a.norm + 2 * row, pack<float, 2>(v));
+    }
     if (a.entropy) a.entropy[row] = r.entropy;
     if (a.logp) a.logp[row] = label_logp(r, y, a.V, xy, a.inv_t);
 }
@@ -310,20 +305,17 @@ __global__ __launch_bounds__(64 * W) void logprobs_long(LogprobArgs a, int split
         Best best{-INFINITY, -1};
         float limit = -INFINITY;
         bool started = false;
-        Run<T, N> next[kU];
+        typename Words<16>::type next[kU];
         auto fetch = [&](int at) {
 #pragma unroll
             for (int u = 0; u < kU; ++u) {
                 const int j = at + (u * 64 + lane) * N;
-                if (j + N <= V) next[u] = *reinterpret_cast<const Run<T, N> *>(x + j);
+                if (j + N <= V) next[u] = load_words<16>(x + j);
                 else {
+                    float part[N];
 #pragma unroll
-                    for (int e = 0; e < N; ++e) next[u].v[e] = j + e < V ? x[j + e] : (T)(sizeof(T) == 2 ? 0xff80 : 0);
-                    if constexpr (sizeof(T) == 4) {
-#pragma unroll
-                        for (int e = 0; e < N; ++e)
-                            if (j + e >= V) next[u].v[e] = -INFINITY;
-                    }
+                    for (int e = 0; e < N; ++e) part[e] = j + e < V ? to_f32(x[j + e]) : -INFINITY;
+                    next[u] = pack<T, N>(part);
                 }
             }
         };
@@ -332,9 +324,7 @@ __global__ __launch_bounds__(64 * W) void logprobs_long(LogprobArgs a, int split
         for (; at < V; at += W * BATCH) {
             float v[kU * N];
 #pragma unroll
-            for (int u = 0; u < kU; ++u)
-#pragma unroll
-                for (int e = 0; e < N; ++e) v[u * N + e] = to_f32(next[u].v[e]);
+            for (int u = 0; u < kU; ++u) unpack<T, N>(next[u], v + u * N);
             if (at + W * BATCH < V) fetch(at + W * BATCH);
             float most[kU], high = -INFINITY;
 #pragma unroll
@@ -474,14 +464,15 @@ struct GradRow {
     bool zero;
     __device__ __forceinline__ GradRow(const LogprobGradArgs &a, int64_t row)
     {
-        const Run<float, 2> nm = *reinterpret_cast<const Run<float, 2> *>(a.norm + 2 * row);
+        float nm[2];
+        load_run<float, 2>(a.norm + 2 * row, nm);
         y = a.labels ? a.labels[row] : -1;
         gl = y >= 0 ? a.g_logp[row] : 0.f;
         ge = a.g_entropy ? a.g_entropy[row] : 0.f;
         ent = a.g_entropy ? a.entropy[row] : 0.f;
         inv_t = a.inv_t;
-        m = y >= a.V ? NAN : nm.v[0];
-        log_s = nm.v[1];
+        m = y >= a.V ? NAN : nm[0];
+        log_s = nm[1];
         zero = m == -INFINITY;
     }
     template <bool EXACT>
@@ -500,10 +491,9 @@ __device__ __forceinline__ void grad_run(const GradRow &r, const T *x, T *g, int
     if (j + N <= V) {
         float v[N];
         load_run<T, N>(x + j, v);
-        Run<T, N> out;
 #pragma unroll
-        for (int e = 0; e < N; ++e) store_as(&out.v[e], r.at<sizeof(T) == 4>(v[e], j + e));
-        *reinterpret_cast<Run<T, N> *>(g + j) = out;
+        for (int e = 0; e < N; ++e) v[e] = r.at<sizeof(T) == 4>(v[e], j + e);
+        store_words<N * sizeof(T)>(g + j, pack<T, N>(v));
     } else {
 #pragma unroll
         for (int e = 0; e < N; ++e)

@@ -44,11 +44,6 @@ __device__ __forceinline__ f4 block_product(const Operand<uint16_t> &a, const Op
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf8, a.v), __builtin_bit_cast(bf8, b.v), c, 0, 0, 0);
 }
 
-template <typename T>
-struct __attribute__((packed, aligned(alignof(T)))) Lane16 {
-    T v[16 / sizeof(T)];
-};
-
 // kE adjacent values at p (any alignment of the element); `have` of them exist,
 // the rest are 0.
 template <typename T>
@@ -56,9 +51,7 @@ __device__ __forceinline__ Operand<T> load_operand(const T *p, int have)
 {
     Operand<T> o;
     if (have >= Operand<T>::kE) {
-        const Lane16<T> r = *reinterpret_cast<const Lane16<T> *>(p);
-#pragma unroll
-        for (int e = 0; e < Operand<T>::kE; ++e) o.v[e] = r.v[e];
+        o.v = __builtin_bit_cast(decltype(o.v), load_words<16>(p));
     } else {
 #pragma unroll
         for (int e = 0; e < Operand<T>::kE; ++e) o.v[e] = e < have ? p[e] : (T)0;
@@ -91,7 +84,7 @@ __device__ __forceinline__ int64_t clamp_row(int64_t row, int64_t rows) { return
 inline int grid_of(int64_t blocks) { return (int)(blocks < 1 ? 1 : blocks > (1 << 22) ? (1 << 22) : blocks); }
 
 // out[rows][cols] = v[rows][C] times the shared matrix w (kernels of
-// project_wide.hip): TRANS false: w [cols][C] (rows' outputs), true: w
+// project_tiles_wide.hip): TRANS false: w [cols][C] (rows' outputs), true: w
 // [C][cols] (rows' gradients); plus t [rows][r] (float32, already scaled for
 // the gradient, times scale[i] otherwise) times the adapter's factor f:
 // [n][cols][r] (TRANS false) or [n][r][cols] (true).

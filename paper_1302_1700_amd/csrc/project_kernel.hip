@@ -4,7 +4,7 @@
 // Few outputs (m + rank up to 64): one pass over the rows, in which the rows
 // of W and of A_i are the columns of one product (project_narrow); more: the
 // rows times A_i first (rank_rows), then a tiled product that adds B_i's part
-// (project_wide.hip).  The factors' gradients: per adapter, sums over its rows
+// (project_tiles_wide.hip).  The factors' gradients: per adapter, sums over its rows
 // of outer products, in runs of rows joined by a second launch in the order of
 // the runs (factor_grad, factor_join).
 #include <algorithm>
@@ -308,10 +308,7 @@ __global__ __launch_bounds__(256) void factor_grad(FactorArgs<T> a)
                     const int c = c0 + b * 64 + q * 4;
                     float vv[4];
                     if (c + 4 <= job.C) {
-                        struct __attribute__((packed, aligned(alignof(T)))) Quad { T v[4]; };
-                        const Quad w = *reinterpret_cast<const Quad *>(v + c);
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) vv[e] = to_f32(w.v[e]);
+                        unpack<T, 4>(load_words<4 * sizeof(T)>(v + c), vv);
                     } else {
 #pragma unroll
                         for (int e = 0; e < 4; ++e) vv[e] = c + e < job.C ? to_f32(v[c + e]) : 0.f;

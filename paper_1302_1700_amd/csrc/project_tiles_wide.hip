@@ -1,0 +1,336 @@
+// The shared projection's matrix product with the adapters' part added to its
+// accumulators: out = v W + t F_i, i the adapter of the row.
+//
+// A workgroup computes a BM x BN tile, its four waves a quarter each.  The
+// summed axis is walked 128 bytes of each row at a time through two LDS
+// buffers: while a step's products run, the next one is written to LDS from
+// registers and the one after that is on its way from memory.  A step is two
+// halves; each half's operands are read while the other half's products run,
+// so one barrier a step suffices and no product waits for LDS.
+//
+// LDS keeps a row's 16-byte pieces in an order turned by the row (piece p of
+// row q at p ^ (q % 8)), so that the 16 rows an operand load touches fall on
+// different banks.  For the gradient of the rows W lies the other way round;
+// its tile keeps the order of memory, and bf16 operands are transposed by the
+// LDS read itself.
+//
+// Blocks are computed as (columns) x (rows): a lane ends up with four adjacent
+// columns of one row, stored together, and has one row's adapter to look at.
+//
+// The adapters' part: for every adapter that a row of the wave names, the
+// product of t with its factor, added only to the rows that name it (an
+// infinity in one adapter stays out of the others' rows).  bf16: t goes in as
+// three bf16 values, each the rounding of what the ones before leave, which
+// keep its 24 bits.
+#include <algorithm>
+#include <type_traits>
+
+#include "project.h"
+
+namespace fs {
+namespace {
+
+typedef short s4 __attribute__((ext_vector_type(4)));
+
+// Tile steps: 128 bytes of the summed axis.
+template <typename T>
+constexpr int kDepth = 128 / sizeof(T);
+
+// Float values as one operand (float32), or three (bf16: what each rounding leaves).
+__device__ __forceinline__ void split_operand(const float *v, Operand<float> *o)
+{
+#pragma unroll
+    for (int e = 0; e < 4; ++e) o[0].v[e] = v[e];
+}
+__device__ __forceinline__ void split_operand(const float *v, Operand<uint16_t> *o)
+{
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        float rest = v[e];
+#pragma unroll
+        for (int p = 0; p < 3; ++p) {
+            o[p].v[e] = to_bf16(rest);
+            rest -= to_f32(o[p].v[e]);
+        }
+    }
+}
+
+template <typename T, bool TRANS, int BM, int BN>
+__global__ __launch_bounds__(256, BM == 256 ? 1 : 2) void project_tiles(WideArgs a, int tiles_m, int tiles_n)
+{
+    constexpr int D = kDepth<T>, E = Operand<T>::kE;
+    static_assert(D == 2 * kStep<T>, "two block products a step");
+    constexpr int WM = BM / 32, WN = BN / 32;                // 16 x 16 blocks of a wave
+    constexpr int PA = BM / 32, PB = BN / 32;                // 16-byte pieces a thread stages
+    constexpr int BP = TRANS ? BN + (sizeof(T) == 2 ? 16 : 4) : 0;  // pitch of W's tile in the order of memory
+    constexpr int A_BYTES = BM * 128, B_BYTES = TRANS ? D * BP * (int)sizeof(T) : BN * 128;
+    __shared__ __align__(16) char lds[2 * (A_BYTES + B_BYTES)];
+
+    // Tiles in the order of the XCDs (workgroup i runs on XCD i % 8): each takes
+    // a run of them, eight tile rows deep, so that its L2 holds their operands.
+    int tile;
+    {
+        const int tiles = tiles_m * tiles_n, per = tiles / 8, more = tiles % 8, xcd = blockIdx.x % 8;
+        tile = xcd * per + min(xcd, more) + blockIdx.x / 8;
+        const int group = 8 * tiles_n, g0 = tile / group * 8, high = min(8, tiles_m - g0), in = tile % group;
+        tile = (g0 + in % high) * tiles_n + in / high;
+    }
+    const int64_t m0 = (int64_t)(tile / tiles_n) * BM;
+    const int n0 = tile % tiles_n * BN;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, q = lane & 15, g = lane >> 4;
+    const int wm = (wave >> 1) * (BM / 2), wn = (wave & 1) * (BN / 2);
+
+    // What the thread stages: pieces of rows (a row's eight pieces by eight
+    // threads), or of W's rows of BN columns; a row or column past the end is
+    // the last one, its products are not stored.
+    constexpr int RPB = BN / E;  // pieces of a row of W as in memory
+    const T *pa[PA], *pb[PB];
+    int kb[PB];                  // TRANS: the piece's row of W
+#pragma unroll
+    for (int i = 0; i < PA; ++i)
+        pa[i] = reinterpret_cast<const T *>(a.v) + clamp_row(m0 + i * 32 + (threadIdx.x >> 3), a.rows) * a.vs + (threadIdx.x & 7) * E;
+#pragma unroll
+    for (int i = 0; i < PB; ++i) {
+        const int piece = i * 256 + threadIdx.x;
+        if constexpr (TRANS) {
+            kb[i] = piece / RPB;
+            int col = n0 + piece % RPB * E;
+            if (a.cols % E == 0) col = min(col, a.cols - E);  // whole pieces lie inside or outside
+            pb[i] = reinterpret_cast<const T *>(a.w) + (int64_t)kb[i] * a.ws + col;
+        } else {
+            kb[i] = 0;
+            pb[i] = reinterpret_cast<const T *>(a.w) + (int64_t)min(n0 + i * 32 + (int)(threadIdx.x >> 3), a.cols - 1) * a.ws +
+                    (threadIdx.x & 7) * E;
+        }
+    }
+    const int step_b = TRANS ? 0 : D;
+    const int64_t step_rows = TRANS ? (int64_t)D * a.ws : 0;
+    typedef decltype(Operand<T>::v) Piece;  // 16 bytes
+    Piece ra[PA], rb[PB];
+    auto fetch = [&](int step) {
+#pragma unroll
+        for (int i = 0; i < PA; ++i) ra[i] = __builtin_bit_cast(Piece, load_words<16>(pa[i] + (int64_t)step * D));
+#pragma unroll
+        for (int i = 0; i < PB; ++i)
+            rb[i] = __builtin_bit_cast(Piece, load_words<16>(pb[i] + (int64_t)step * step_b + step * step_rows));
+    };
+    // the last step's terms past the end are 0, and W's columns past the end stay unread
+    auto fetch_checked = [&](int step) {
+        const int c0 = step * D;
+#pragma unroll
+        for (int i = 0; i < PA; ++i) ra[i] = load_operand(pa[i] + c0, a.C - c0 - (int)(threadIdx.x & 7) * E).v;
+#pragma unroll
+        for (int i = 0; i < PB; ++i) {
+            if constexpr (TRANS) {
+                const int have = a.cols % E == 0 ? E : a.cols - (n0 + (i * 256 + (int)threadIdx.x) % RPB * E);
+                rb[i] = load_operand(pb[i] + step * step_rows, c0 + kb[i] < a.C ? have : 0).v;
+            } else {
+                rb[i] = load_operand(pb[i] + c0, a.C - c0 - (int)(threadIdx.x & 7) * E).v;
+            }
+        }
+    };
+    auto put = [&](int at) {
+        char *la = lds + at * (A_BYTES + B_BYTES), *lb = la + A_BYTES;
+        const int turned = (threadIdx.x >> 3) * 128 + (((threadIdx.x & 7) ^ (threadIdx.x >> 3 & 7)) << 4);
+#pragma unroll
+        for (int i = 0; i < PA; ++i)
+            *reinterpret_cast<Piece *>(la + i * 4096 + turned) = ra[i];
+#pragma unroll
+        for (int i = 0; i < PB; ++i) {
+            const int piece = i * 256 + threadIdx.x;
+            char *to = TRANS ? lb + (piece / RPB * BP + piece % RPB * E) * (int)sizeof(T) : lb + i * 4096 + turned;
+            *reinterpret_cast<Piece *>(to) = rb[i];
+        }
+    };
+    f4 acc[WM][WN];
+#pragma unroll
+    for (int i = 0; i < WM; ++i)
+#pragma unroll
+        for (int j = 0; j < WN; ++j) acc[i][j] = f4{0.f, 0.f, 0.f, 0.f};
+
+    auto read = [&](int at, int half, Operand<T>(&oa)[WM], Operand<T>(&ob)[WN]) {
+        const char *la = lds + at * (A_BYTES + B_BYTES), *lb = la + A_BYTES;
+        const int turned = q * 128 + (((half * 4 + g) ^ (q & 7)) << 4);
+#pragma unroll
+        for (int i = 0; i < WM; ++i)
+            oa[i] = *reinterpret_cast<const Operand<T> *>(la + (wm + i * 16) * 128 + turned);
+#pragma unroll
+        for (int j = 0; j < WN; ++j) {
+            if constexpr (!TRANS) {
+                ob[j] = *reinterpret_cast<const Operand<T> *>(lb + (wn + j * 16) * 128 + turned);
+            } else if constexpr (sizeof(T) == 4) {
+                const float *b = reinterpret_cast<const float *>(lb) + (half * 16 + g * 4) * BP + wn + j * 16 + q;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) ob[j].v[e] = b[e * BP];
+            } else {
+                // 16 lanes read four rows of 16 columns, four columns a lane, and get a column each
+                const uint16_t *b = reinterpret_cast<const uint16_t *>(lb) + (half * 32 + g * 8 + (q >> 2)) * BP + wn +
+                                    j * 16 + (q & 3) * 4;
+                const s4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s4 *)(b));
+                const s4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s4 *)(b + 4 * BP));
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    ob[j].v[e] = (uint16_t)lo[e];
+                    ob[j].v[e + 4] = (uint16_t)hi[e];
+                }
+            }
+        }
+    };
+    auto products = [&](const Operand<T>(&oa)[WM], const Operand<T>(&ob)[WN]) {
+#pragma unroll
+        for (int i = 0; i < WM; ++i)
+#pragma unroll
+            for (int j = 0; j < WN; ++j) acc[i][j] = block_product(ob[j], oa[i], acc[i][j]);
+    };
+
+    const int steps = (a.C + D - 1) / D;
+    // steps that are read without checks
+    const int whole = TRANS && a.cols % E != 0 && n0 + BN > a.cols ? 0 : a.C / D;
+    auto get = [&](int step) {
+        if (step < whole) fetch(step);
+        else if (step < steps) fetch_checked(step);
+    };
+    get(0);
+    put(0);
+    get(1);
+    __syncthreads();
+    Operand<T> oa[2][WM], ob[2][WN];
+    read(0, 0, oa[0], ob[0]);
+    int s = 0;
+    for (; s + 2 < whole; ++s) {
+        put((s + 1) & 1);
+        fetch(s + 2);
+        read(s & 1, 1, oa[1], ob[1]);
+        products(oa[0], ob[0]);
+        __syncthreads();
+        read((s + 1) & 1, 0, oa[0], ob[0]);
+        products(oa[1], ob[1]);
+    }
+    for (; s < steps; ++s) {
+        if (s + 1 < steps) put((s + 1) & 1);
+        get(s + 2);
+        read(s & 1, 1, oa[1], ob[1]);
+        products(oa[0], ob[0]);
+        __syncthreads();
+        if (s + 1 < steps) read((s + 1) & 1, 0, oa[0], ob[0]);
+        products(oa[1], ob[1]);
+    }
+
+    // the adapters' part
+    int id[WM];
+#pragma unroll
+    for (int i = 0; i < WM; ++i) {
+        const int64_t row = m0 + wm + i * 16 + q;
+        id[i] = a.n && row < a.rows ? a.ids[row] : -1;
+    }
+    if (a.n) {
+        for (int last = -1;;) {
+            int low = 0x7fffffff;
+#pragma unroll
+            for (int i = 0; i < WM; ++i) low = id[i] > last ? min(low, id[i]) : low;
+            const int cur = next_adapter(low, last);
+            if (cur >= a.n) break;
+            last = cur;
+            const float sc = !TRANS && a.scale ? a.scale[cur] : 1.f;
+            const T *f = reinterpret_cast<const T *>(a.f) + (int64_t)cur * a.cols * a.r;
+            constexpr int Q = sizeof(T) == 2 ? 3 : 1;
+#pragma unroll
+            for (int i = 0; i < WM; ++i) {
+                if (!__any(id[i] == cur)) continue;
+                f4 z[WN];
+#pragma unroll
+                for (int j = 0; j < WN; ++j) z[j] = f4{0.f, 0.f, 0.f, 0.f};
+                const float *t = a.t + clamp_row(m0 + wm + i * 16 + q, a.rows) * a.r;
+                for (int k0 = 0; k0 < a.r; k0 += kStep<T>) {
+                    const int k = k0 + g * E;
+                    float tv[E];
+#pragma unroll
+                    for (int e = 0; e < E; ++e) tv[e] = k + e < a.r ? t[k + e] * sc : 0.f;
+                    Operand<T> ot[Q];
+                    split_operand(tv, ot);
+#pragma unroll
+                    for (int j = 0; j < WN; ++j) {
+                        const int col = min(n0 + wn + j * 16 + q, a.cols - 1);
+                        const Operand<T> of = TRANS ? gather_operand(f + (int64_t)k * a.cols + col, a.cols, a.r - k)
+                                                    : load_operand(f + (int64_t)col * a.r + k, a.r - k);
+#pragma unroll
+                        for (int p = 0; p < Q; ++p) z[j] = block_product(of, ot[p], z[j]);
+                    }
+                }
+                const bool hit = id[i] == cur;
+#pragma unroll
+                for (int j = 0; j < WN; ++j)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) acc[i][j][e] += hit ? z[j][e] : 0.f;
+            }
+        }
+    }
+
+#pragma unroll
+    for (int j = 0; j < WN; ++j) {
+        const int col = n0 + wn + j * 16 + g * 4;
+        float bias[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) bias[e] = a.bias && col + e < a.cols ? a.bias[col + e] : 0.f;
+#pragma unroll
+        for (int i = 0; i < WM; ++i) {
+            const int64_t row = m0 + wm + i * 16 + q;
+            if (row >= a.rows) continue;
+            float out[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) out[e] = a.n && id[i] >= a.n ? NAN : acc[i][j][e] + bias[e];
+            T *to = reinterpret_cast<T *>(a.out) + row * a.os + col;
+            if (col + 4 <= a.cols) store_words<4 * sizeof(T)>(to, pack<T, 4>(out));
+            else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (col + e < a.cols) store_as(to + e, out[e]);
+            }
+        }
+    }
+}
+
+template <typename T, bool TRANS, int BM, int BN>
+hipError_t go(const WideArgs &a, hipStream_t s)
+{
+    const int64_t tm = (a.rows + BM - 1) / BM;
+    const int tn = (a.cols + BN - 1) / BN;
+    // a launch holds fewer than 2^24 workgroups: more rows in several
+    const int64_t most = std::max<int64_t>(1, (1 << 22) / tn);
+    for (int64_t at = 0; at < tm; at += most) {
+        WideArgs p = a;
+        const int64_t m = std::min(most, tm - at), row = at * BM;
+        p.v = (const T *)a.v + row * a.vs;
+        p.out = (T *)a.out + row * a.os;
+        p.rows = a.rows - row;
+        if (at + m < tm) p.rows = std::min<int64_t>(p.rows, m * BM);
+        if (a.n) {
+            p.t = a.t + row * a.r;
+            p.ids = a.ids + row;
+        }
+        hipLaunchKernelGGL((project_tiles<T, TRANS, BM, BN>), dim3((unsigned)(m * tn)), dim3(256), 0, s, p, (int)m, tn);
+        hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
+}
+
+template <typename T, bool TRANS>
+hipError_t choose(const WideArgs &a, hipStream_t s)
+{
+    const auto tiles = [&](int b) { return ((a.rows + b - 1) / b) * ((a.cols + b - 1) / b); };
+    if constexpr (sizeof(T) == 2)
+        if (tiles(256) < 0) return go<T, TRANS, 256, 256>(a, s);
+    if (tiles(128) >= 256) return go<T, TRANS, 128, 128>(a, s);
+    return go<T, TRANS, 64, 64>(a, s);
+}
+
+}  // namespace
+
+hipError_t launch_wide(const WideArgs &a, int dtype, bool trans, hipStream_t s)
+{
+    if (dtype == DT_BF16) return trans ? choose<uint16_t, true>(a, s) : choose<uint16_t, false>(a, s);
+    return trans ? choose<float, true>(a, s) : choose<float, false>(a, s);
+}
+
+}  // namespace fs

@@ -68,4 +68,49 @@ __device__ __forceinline__ uint16_t to_bf16(float f)
 __device__ __forceinline__ void store_as(float *p, float v) { *p = v; }
 __device__ __forceinline__ void store_as(uint16_t *p, float v) { *p = to_bf16(v); }
 
+// 4, 8 or 16 adjacent bytes at an address of any alignment its elements may
+// have: one load or store (as an array of 16-bit elements the compiler takes
+// it apart).
+template <int BYTES>
+struct Words {
+    typedef uint32_t type __attribute__((ext_vector_type(BYTES / 4)));
+    typedef uint32_t at2 __attribute__((ext_vector_type(BYTES / 4), aligned(2)));
+    typedef uint32_t at4 __attribute__((ext_vector_type(BYTES / 4), aligned(4)));
+};
+template <int BYTES, typename T>
+__device__ __forceinline__ typename Words<BYTES>::type load_words(const T *p)
+{
+    if constexpr (sizeof(T) == 2) return *reinterpret_cast<const typename Words<BYTES>::at2 *>(p);
+    else return *reinterpret_cast<const typename Words<BYTES>::at4 *>(p);
+}
+template <int BYTES, typename T>
+__device__ __forceinline__ void store_words(T *p, typename Words<BYTES>::type v)
+{
+    if constexpr (sizeof(T) == 2) *reinterpret_cast<typename Words<BYTES>::at2 *>(p) = v;
+    else *reinterpret_cast<typename Words<BYTES>::at4 *>(p) = v;
+}
+// The N elements of such words as float32, and back.
+template <typename T, int N, typename W>
+__device__ __forceinline__ void unpack(W w, float *v)
+{
+#pragma unroll
+    for (int e = 0; e < N; ++e) {
+        if constexpr (sizeof(T) == 4) v[e] = __uint_as_float(w[e]);
+        else v[e] = __uint_as_float(e & 1 ? w[e / 2] & 0xffff0000u : w[e / 2] << 16);
+    }
+}
+template <typename T, int N>
+__device__ __forceinline__ typename Words<N * sizeof(T)>::type pack(const float *v)
+{
+    typename Words<N * sizeof(T)>::type w;
+    if constexpr (sizeof(T) == 4) {
+#pragma unroll
+        for (int e = 0; e < N; ++e) w[e] = __float_as_uint(v[e]);
+    } else {
+#pragma unroll
+        for (int e = 0; e < N / 2; ++e) w[e] = (uint32_t)to_bf16(v[2 * e]) | (uint32_t)to_bf16(v[2 * e + 1]) << 16;
+    }
+    return w;
+}
+
 }  // namespace fs
