@@ -95,7 +95,9 @@ struct WideArgs {
     int C, cols, n, r;
     const float *bias, *scale, *t;
     const int *ids;
+    float *parts;  // wide_parts() bytes: where the summed axis is split
 };
+size_t wide_parts(int64_t rows, int cols, int C, int dtype);
 hipError_t launch_wide(const WideArgs &a, int dtype, bool trans, hipStream_t s);
 
 }  // namespace fs

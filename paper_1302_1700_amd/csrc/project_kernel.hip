@@ -52,75 +52,112 @@ __device__ __forceinline__ void row_products(const T *const (&row)[RB], const T 
     }
 }
 
-// Rows times a factor, t[row][j] = s_i sum_c v[row][c] f_i[j][c]: f [n][r][C]
-// (TRANS false: A) or [n][C][r] (true: B).  A wave takes 16 rows, W waves share
-// the summed axis of them.
-template <typename T, int NB, int W, bool TRANS>
-__global__ __launch_bounds__(256) void rank_rows(const T *v, int64_t vs, int64_t rows, int C, const T *f, int n, int r,
-                                                 const float *scale, const int *ids, float *t)
+// The rows of one adapter among 1024: their offsets from the first, in order, in
+// `list`; returns how many.  All threads of the workgroup take part (NW waves);
+// `id` is called with every row's adapter once: id(row, adapter).
+template <int NW, typename Each>
+__device__ __forceinline__ int list_rows(const int *ids, int64_t at, int64_t end, int adapter, int *list, int *count,
+                                         Each each)
 {
-    __shared__ float part[W > 1 ? 4 * 16 * NB * 16 : 1];
+    constexpr int G = 16 / NW > 0 ? 16 / NW : 1;  // groups of 64 ids a wave looks at
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    uint64_t who[G];
+    __syncthreads();  // the list before has been read
+#pragma unroll
+    for (int k = 0; k < G; ++k) {
+        const int64_t row = at + (wave * G + k) * 64 + lane;
+        const int id = row < end ? ids[row] : -1;
+        if (row < end) each(row, id);
+        who[k] = __ballot(row < end && id == adapter);
+        if (lane == 0) count[wave * G + k] = __popcll(who[k]);
+    }
+    __syncthreads();
+    int total = 0, before = 0;
+#pragma unroll
+    for (int k = 0; k < 16; ++k) {
+        if (k < wave * G) before += count[k];
+        total += count[k];
+    }
+#pragma unroll
+    for (int k = 0; k < G; ++k) {
+        if (who[k] >> lane & 1) list[before + __popcll(who[k] & ((1ull << lane) - 1))] = (wave * G + k) * 64 + lane;
+        before += __popcll(who[k]);
+    }
+    __syncthreads();
+    return total;
+}
+
+// Rows times their adapter's factor, t[row][j] = s_i sum_c v[row][c] f_i[j][c]:
+// f [n][r][C] (TRANS false: A) or [n][C][r] (true: B).  A workgroup takes one
+// adapter's rows among 1024, 16 to a product, so that mixed rows cost no more
+// products than sorted ones; workgroups with different `slot` take different
+// sixteens.  W waves share the summed axis of a product.
+template <typename T>
+struct RankArgs {
+    const T *v, *f;
+    int64_t vs, rows;
+    int C, n, r, slots;
+    const float *scale;
+    const int *ids;
+    float *t;
+};
+
+template <typename T, int NB, int W, bool TRANS>
+__global__ __launch_bounds__(W == 16 ? 1024 : 256) void rank_rows(RankArgs<T> a)
+{
+    constexpr int NW = W == 16 ? 16 : 4, PER = NW / W;
+    __shared__ float part[W > 1 ? W * 256 : 1];
+    __shared__ int list[1024], count[16];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, q = lane & 15, g = lane >> 4;
-    const int64_t tiles = (rows + 15) / 16;
-    constexpr int PER = 4 / W;  // tiles of a workgroup
-    for (int64_t tile0 = (int64_t)blockIdx.x * PER; tile0 < tiles; tile0 += (int64_t)gridDim.x * PER) {
-        const int64_t row0 = (tile0 + wave / W) * 16;
-        const int id = row0 + q < rows ? ids[row0 + q] : -1;
-        const T *row[1] = {v + clamp_row(row0 + q, rows) * vs};
+    const int n = a.n, r = a.r;
+    const int64_t units = (a.rows + 1023) / 1024 * n;
+    for (int64_t unit = blockIdx.y; unit < units; unit += gridDim.y) {
+        const int64_t chunk = unit / n, at = chunk * 1024;
+        const int i = (int)(unit - chunk * n);
+        const bool others = i == 0 && blockIdx.x == 0;  // this workgroup also writes the rows without an adapter
+        const int total = list_rows<NW>(a.ids, at, a.rows, i, list, count, [&](int64_t row, int id) {
+            if (others && (id < 0 || id >= n))
+                for (int j = 0; j < r; ++j) a.t[row * r + j] = id < 0 ? 0.f : NAN;
+        });
+        const float sc = a.scale ? a.scale[i] : 1.f;
         constexpr int S = kStep<T>;
-        const int run = W == 1 ? C : (C + W * S - 1) / (W * S) * S;
-        const int c0 = std::min(C, wave % W * run), c1 = std::min(C, c0 + run);
-        float out[NB][4];
-#pragma unroll
-        for (int j = 0; j < NB; ++j)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) out[j][e] = 0.f;
-        for (int last = -1;;) {
-            const int cur = next_adapter(id, last);
-            if (cur >= n) break;
-            last = cur;
+        const int run = W == 1 ? a.C : (a.C + W * S - 1) / (W * S) * S;
+        const int c0 = std::min(a.C, wave % W * run), c1 = std::min(a.C, c0 + run);
+        for (int tile = blockIdx.x * PER + wave / W; tile * 16 < total; tile += a.slots * PER) {
+            const T *row[1] = {a.v + (at + list[std::min(tile * 16 + q, total - 1)]) * a.vs};
             const T *col[NB];
             f4 acc[1][NB];
 #pragma unroll
             for (int j = 0; j < NB; ++j) {
                 const int c = j * 16 + q;
-                col[j] = c >= r ? nullptr : TRANS ? f + (int64_t)cur * r * C + c : f + ((int64_t)cur * r + c) * C;
+                col[j] = c >= r ? nullptr : TRANS ? a.f + (int64_t)i * r * a.C + c : a.f + ((int64_t)i * r + c) * a.C;
                 acc[0][j] = f4{0.f, 0.f, 0.f, 0.f};
             }
             row_products<TRANS, T, 1, NB>(row, col, r, c0, c1, acc);
-            if constexpr (W > 1) {
-                __syncthreads();
 #pragma unroll
-                for (int j = 0; j < NB; ++j)
+            for (int j = 0; j < NB; ++j) {
+                if constexpr (W > 1) {
+                    __syncthreads();
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) part[((wave * NB + j) * 4 + e) * 64 + lane] = acc[0][j][e];
-                __syncthreads();
+                    for (int e = 0; e < 4; ++e) part[wave * 256 + e * 64 + lane] = acc[0][j][e];
+                    __syncthreads();
+                    if (wave == 0) {
 #pragma unroll
-                for (int j = 0; j < NB; ++j)
+                        for (int e = 0; e < 4; ++e) {
+                            float s = 0.f;
+#pragma unroll
+                            for (int k = 0; k < W; ++k) s += part[k * 256 + e * 64 + lane];
+                            acc[0][j][e] = s;
+                        }
+                    }
+                }
+                if (wave % W == 0) {
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        float s = 0.f;
-#pragma unroll
-                        for (int k = 0; k < W; ++k) s += part[((k * NB + j) * 4 + e) * 64 + lane];
-                        acc[0][j][e] = s;
+                        const int k = tile * 16 + g * 4 + e;
+                        if (k < total && j * 16 + q < r) a.t[(at + list[k]) * r + j * 16 + q] = acc[0][j][e] * sc;
                     }
-            }
-            const float sc = scale ? scale[cur] : 1.f;
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-                if (__shfl(id, g * 4 + e) == cur) {
-#pragma unroll
-                    for (int j = 0; j < NB; ++j) out[j][e] = acc[0][j][e] * sc;
                 }
-        }
-        if (wave % W == 0) {
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int64_t to = row0 + g * 4 + e;
-                const bool bad = __shfl(id, g * 4 + e) >= n;
-#pragma unroll
-                for (int j = 0; j < NB; ++j)
-                    if (to < rows && j * 16 + q < r) t[to * r + j * 16 + q] = bad ? NAN : out[j][e];
             }
         }
     }
@@ -130,13 +167,13 @@ __global__ __launch_bounds__(256) void rank_rows(const T *v, int64_t vs, int64_t
 // A_i's; the products go through LDS, where each row's outputs take up their
 // hidden values.  A wave takes 16 RB rows (W = 1), or 16 shared by W waves.
 template <typename T, int RB, int NB, int W>
-__global__ __launch_bounds__(256) void project_narrow(ProjArgs a, T *y, int64_t ys, float *hidden)
+__global__ __launch_bounds__(W == 16 ? 1024 : 256) void project_narrow(ProjArgs a, T *y, int64_t ys, float *hidden)
 {
-    constexpr int P = NB * 16 + 1;
-    __shared__ float part[4][16 * RB][P];
+    constexpr int P = NB * 16 + 1, NW = W == 16 ? 16 : 4;
+    __shared__ float part[NW][16 * RB][P];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, q = lane & 15, g = lane >> 4;
     const int64_t tiles = (a.rows + 16 * RB - 1) / (16 * RB);
-    constexpr int PER = 4 / W;
+    constexpr int PER = NW / W;
     const T *x = (const T *)a.x, *w = (const T *)a.w, *fa = (const T *)a.a, *fb = (const T *)a.b;
     const int M = a.M, r = a.r, n = a.n;
     for (int64_t tile0 = (int64_t)blockIdx.x * PER; tile0 < tiles; tile0 += (int64_t)gridDim.x * PER) {
@@ -175,7 +212,7 @@ __global__ __launch_bounds__(256) void project_narrow(ProjArgs a, T *y, int64_t 
                     for (int e = 0; e < 4; ++e) part[wave][i * 16 + g * 4 + e][j * 16 + q] = acc[i][j][e];
             if (W > 1) {
                 __syncthreads();
-                for (int k = threadIdx.x; k < 16 * RB * (M + r); k += 256) {
+                for (int k = threadIdx.x; k < 16 * RB * (M + r); k += 64 * NW) {
                     const int rr = k / (M + r), c = k - rr * (M + r);
                     float s = part[0][rr][c];
 #pragma unroll
@@ -239,22 +276,67 @@ struct FactorArgs {
     int run_rows, runs, n, r;
     const int *ids;
     uint8_t *used;  // [n][runs]: the run holds rows of the adapter
+    const T *b;     // factor_both: [n][M][r]
 };
 
-// Columns of a workgroup: 64 KB' worth of accumulators, 16 ranks a block.
+// Columns of a workgroup: 64 accumulators' worth, 16 ranks a block.
 template <int NB>
 constexpr int kFactorCols = NB == 1 ? 256 : NB == 2 ? 128 : 64;
 
+// Four adjacent values of a row from column c on, 0 past its C columns.
+template <typename T>
+__device__ __forceinline__ void four(const T *v, int c, int C, float (&vv)[4])
+{
+    if (c + 4 <= C) unpack<T, 4>(load_words<4 * sizeof(T)>(v + c), vv);
+    else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) vv[e] = c + e < C ? to_f32(v[c + e]) : 0.f;
+    }
+}
+
+// Where a sum goes: the part of a run, or the gradient itself when there is one run.
+template <typename T>
+__device__ __forceinline__ void store_sum(const FactorArgs<T> &a, const FactorJob<T> &job, int64_t unit, int i, int j, int c,
+                                          float s)
+{
+    if (j >= a.r || c >= job.C) return;
+    if (a.runs > 1) job.parts[(unit * a.r + j) * job.C + c] = s;
+    else
+        store_as(job.out + (job.by_rank ? ((int64_t)i * a.r + j) * job.C + c : ((int64_t)i * job.C + c) * a.r + j),
+                 job.scale ? s * job.scale[i] : s);
+}
+
+// Joins the four waves' blocks and stores them; element e of lane l: rank
+// 16 j + 4 (l / 16) + e, column `c` of l % 16.
+template <typename T, int NB, typename Column>
+__device__ __forceinline__ void store_blocks(const FactorArgs<T> &a, const FactorJob<T> &job, int64_t unit, int i,
+                                             const f4 (&acc)[NB], float (*sums)[64][NB * 4 + 1], Column column)
+{
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < NB; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sums[wave][lane][j * 4 + e] = acc[j][e];
+    __syncthreads();
+    for (int k = threadIdx.x; k < 64 * NB * 4; k += 256) {
+        const int l = k & 63, je = k >> 6;
+        const float s = (sums[0][l][je] + sums[1][l][je]) + (sums[2][l][je] + sums[3][l][je]);
+        store_sum(a, job, unit, i, je / 4 * 16 + (l >> 4) * 4 + je % 4, column(l & 15), s);
+    }
+}
+
 // Workgroup: one adapter, one run of rows, one tile of columns.  The run's rows
 // that name the adapter are listed in LDS, 1024 ids at a time; the four waves
-// take four listed rows each in turn as the summed axis of float32 products
-// (bf16 values are exact in them).
+// take kGroups times four listed rows each in turn as the summed axis of
+// float32 products (bf16 values are exact in them).
+constexpr int kGroups = 2;
+
 template <typename T, int NB>
 __global__ __launch_bounds__(256) void factor_grad(FactorArgs<T> a)
 {
     constexpr int CT = kFactorCols<NB>, CB = CT / 64;
-    __shared__ int list[1024 + 16];
-    __shared__ int count[17];
+    __shared__ int list[1024], count[16];
     __shared__ float sums[4][64][NB * 4 + 1];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, q = lane & 15, g = lane >> 4;
     const int which = blockIdx.x >= (unsigned)a.job[0].ctiles;
@@ -271,100 +353,140 @@ __global__ __launch_bounds__(256) void factor_grad(FactorArgs<T> a)
             for (int j = 0; j < NB; ++j) acc[b][j] = f4{0.f, 0.f, 0.f, 0.f};
         bool seen = false;
         for (int64_t at = begin; at < end; at += 1024) {
-            // the listed rows, in their order: sixteen groups of 64 ids
-            __syncthreads();
-            uint64_t who[4];
+            const int total = list_rows<4>(a.ids, at, end, i, list, count, [](int64_t, int) {});
+            seen |= total > 0;
+            for (int l = wave * 4 * kGroups; l < total; l += 16 * kGroups) {
+                float tv[kGroups][NB], vv[kGroups][CB][4];
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                const int64_t row = at + (wave * 4 + k) * 64 + lane;
-                who[k] = __ballot(row < end && a.ids[std::min(row, a.rows - 1)] == i);
-                if (lane == 0) count[wave * 4 + k] = __popcll(who[k]);
-            }
-            __syncthreads();
-            int total = 0, before = 0;
+                for (int k = 0; k < kGroups; ++k) {
+                    const bool have = l + k * 4 + g < total;
+                    const int64_t row = at + list[have ? l + k * 4 + g : l];
 #pragma unroll
-            for (int k = 0; k < 16; ++k) {
-                if (k < wave * 4) before += count[k];
-                total += count[k];
-            }
-            if (total == 0) continue;
-            seen = true;
+                    for (int j = 0; j < NB; ++j)
+                        tv[k][j] = have && j * 16 + q < r ? job.t[row * r + j * 16 + q] : 0.f;
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                const int below = __popcll(who[k] & ((1ull << lane) - 1));
-                if (who[k] >> lane & 1) list[before + below] = (wave * 4 + k) * 64 + lane;
-                before += __popcll(who[k]);
-            }
-            __syncthreads();
-            for (int l = wave * 4; l < total; l += 16) {
-                const bool have = l + g < total;
-                const int64_t row = at + list[have ? l + g : l];
-                float tv[NB];
-#pragma unroll
-                for (int j = 0; j < NB; ++j) tv[j] = have && j * 16 + q < r ? job.t[row * r + j * 16 + q] : 0.f;
-                const T *v = job.v + row * job.vs;
-#pragma unroll
-                for (int b = 0; b < CB; ++b) {
-                    const int c = c0 + b * 64 + q * 4;
-                    float vv[4];
-                    if (c + 4 <= job.C) {
-                        unpack<T, 4>(load_words<4 * sizeof(T)>(v + c), vv);
-                    } else {
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) vv[e] = c + e < job.C ? to_f32(v[c + e]) : 0.f;
+                    for (int b = 0; b < CB; ++b) {
+                        four(job.v + row * job.vs, c0 + b * 64 + q * 4, job.C, vv[k][b]);
+                        if (!have) vv[k][b][0] = vv[k][b][1] = vv[k][b][2] = vv[k][b][3] = 0.f;
                     }
+                }
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const float ve = have ? vv[e] : 0.f;
+                for (int k = 0; k < kGroups; ++k)
 #pragma unroll
-                        for (int j = 0; j < NB; ++j)
-                            acc[b * 4 + e][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(tv[j], ve, acc[b * 4 + e][j], 0, 0, 0);
+                    for (int b = 0; b < CB; ++b)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+#pragma unroll
+                            for (int j = 0; j < NB; ++j)
+                                acc[b * 4 + e][j] =
+                                    __builtin_amdgcn_mfma_f32_16x16x4f32(tv[k][j], vv[k][b][e], acc[b * 4 + e][j], 0, 0, 0);
+            }
+        }
+        if (threadIdx.x == 0 && blockIdx.x == 0 && a.used) a.used[unit] = seen;
+        if (!seen && a.runs > 1) continue;
+#pragma unroll
+        for (int bp = 0; bp < CB * 4; ++bp)
+            store_blocks<T, NB>(a, job, unit, i, acc[bp], sums,
+                                [&](int l) { return c0 + (bp >> 2) * 64 + l * 4 + (bp & 3); });
+    }
+}
+
+// Few outputs and ranks (M and r up to 16): both factors' gradients in one pass
+// over the rows.  A lane holds column q of its adapter's B and makes u = B^T g
+// of its row from the row's 16 lanes, so u never goes through memory.
+template <typename T>
+__global__ __launch_bounds__(256) void factor_both(FactorArgs<T> a)
+{
+    constexpr int CB = 4;
+    __shared__ int list[1024], count[16];
+    __shared__ float sums[4][64][5];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, q = lane & 15, g = lane >> 4;
+    const FactorJob<T> &ja = a.job[0], &jb = a.job[1];
+    const int c0 = (int)blockIdx.x * 256, r = a.r, M = jb.C;
+    for (int64_t unit = blockIdx.y; unit < (int64_t)a.n * a.runs; unit += gridDim.y) {
+        const int i = (int)(unit / a.runs), run = (int)(unit - (int64_t)i * a.runs);
+        const int64_t begin = (int64_t)run * a.run_rows, end = std::min(a.rows, begin + a.run_rows);
+        const float sc = jb.scale ? jb.scale[i] : 1.f;
+        float bi[16];
+#pragma unroll
+        for (int m = 0; m < 16; ++m) bi[m] = m < M && q < r ? to_f32(a.b[((int64_t)i * M + m) * r + q]) * sc : 0.f;
+        f4 acc[CB * 4], gb = f4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int b = 0; b < CB * 4; ++b) acc[b] = f4{0.f, 0.f, 0.f, 0.f};
+        bool seen = false;
+        for (int64_t at = begin; at < end; at += 1024) {
+            const int total = list_rows<4>(a.ids, at, end, i, list, count, [](int64_t, int) {});
+            seen |= total > 0;
+            for (int l = wave * 4 * kGroups; l < total; l += 16 * kGroups) {
+                float hv[kGroups], gv[kGroups], vv[kGroups][CB][4];
+#pragma unroll
+                for (int k = 0; k < kGroups; ++k) {
+                    const bool have = l + k * 4 + g < total;
+                    const int64_t row = at + list[have ? l + k * 4 + g : l];
+                    gv[k] = have && q < M ? to_f32(jb.v[row * jb.vs + q]) : 0.f;
+                    hv[k] = have && q < r ? jb.t[row * r + q] : 0.f;
+#pragma unroll
+                    for (int b = 0; b < CB; ++b) {
+                        four(ja.v + row * ja.vs, c0 + b * 64 + q * 4, ja.C, vv[k][b]);
+                        if (!have) vv[k][b][0] = vv[k][b][1] = vv[k][b][2] = vv[k][b][3] = 0.f;
                     }
+                }
+#pragma unroll
+                for (int k = 0; k < kGroups; ++k) {
+                    float u = 0.f;
+#pragma unroll
+                    for (int m = 0; m < 16; ++m)
+                        if (m < M) u = fmaf(__shfl(gv[k], (lane & 48) + m), bi[m], u);
+                    gb = __builtin_amdgcn_mfma_f32_16x16x4f32(hv[k], gv[k], gb, 0, 0, 0);
+#pragma unroll
+                    for (int b = 0; b < CB; ++b)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            acc[b * 4 + e] = __builtin_amdgcn_mfma_f32_16x16x4f32(u, vv[k][b][e], acc[b * 4 + e], 0, 0, 0);
                 }
             }
         }
         if (threadIdx.x == 0 && blockIdx.x == 0 && a.used) a.used[unit] = seen;
         if (!seen && a.runs > 1) continue;
-        // the waves' sums joined block by block; ranks 16 j + 4 g + e, column 64 b + 4 q + p
-        const float sc = job.scale ? job.scale[i] : 1.f;
 #pragma unroll
         for (int bp = 0; bp < CB * 4; ++bp) {
-            __syncthreads();
-#pragma unroll
-            for (int j = 0; j < NB; ++j)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) sums[wave][lane][j * 4 + e] = acc[bp][j][e];
-            __syncthreads();
-            for (int k = threadIdx.x; k < 64 * NB * 4; k += 256) {
-                const int l = k & 63, je = k >> 6;
-                const float s = sums[0][l][je] + sums[1][l][je] + sums[2][l][je] + sums[3][l][je];
-                const int j = je / 4 * 16 + (l >> 4) * 4 + je % 4, c = c0 + (bp >> 2) * 64 + (l & 15) * 4 + (bp & 3);
-                if (j >= r || c >= job.C) continue;
-                if (a.runs > 1) job.parts[((unit * r) + j) * job.C + c] = s;
-                else {
-                    const int64_t o = job.by_rank ? ((int64_t)i * r + j) * job.C + c : ((int64_t)i * job.C + c) * r + j;
-                    store_as(job.out + o, s * sc);
-                }
-            }
+            const f4 one[1] = {acc[bp]};
+            store_blocks<T, 1>(a, ja, unit, i, one, sums, [&](int l) { return c0 + (bp >> 2) * 64 + l * 4 + (bp & 3); });
+        }
+        if (blockIdx.x == 0) {
+            const f4 one[1] = {gb};
+            store_blocks<T, 1>(a, jb, unit, i, one, sums, [&](int l) { return l; });
         }
     }
 }
 
-// Sums the runs' parts in the order of the runs.
+// Sums the runs' parts: 64 values to a workgroup, each wave a quarter of the
+// runs in their order, the quarters joined in order.
 template <typename T>
 __global__ __launch_bounds__(256) void factor_join(FactorArgs<T> a)
 {
+    __shared__ float sums[4][64];
     const FactorJob<T> &job = a.job[blockIdx.y];
-    const int64_t total = (int64_t)a.n * a.r * job.C;
-    for (int64_t k = (int64_t)blockIdx.x * 256 + threadIdx.x; k < total; k += (int64_t)gridDim.x * 256) {
-        const int c = (int)(k % job.C), j = (int)(k / job.C % a.r), i = (int)(k / job.C / a.r);
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int per_adapter = a.r * job.C, blocks = (per_adapter + 63) / 64;
+    const int quarter = (a.runs + 3) / 4, from = wave * quarter, to = std::min(a.runs, from + quarter);
+    for (int64_t unit = blockIdx.x; unit < (int64_t)a.n * blocks; unit += gridDim.x) {
+        const int i = (int)(unit / blocks), k = (int)(unit - (int64_t)i * blocks) * 64 + lane;
+        const uint8_t *used = a.used + (int64_t)i * a.runs;
+        const float *parts = job.parts + (int64_t)i * a.runs * per_adapter;
         float s = 0.f;
-        for (int run = 0; run < a.runs; ++run) {
-            const int64_t unit = (int64_t)i * a.runs + run;
-            if (a.used[unit]) s += job.parts[(unit * a.r + j) * job.C + c];
+        if (k < per_adapter)
+            for (int run = from; run < to; ++run)
+                if (used[run]) s += parts[(int64_t)run * per_adapter + k];
+        __syncthreads();
+        sums[wave][lane] = s;
+        __syncthreads();
+        if (wave == 0 && k < per_adapter) {
+            s = (sums[0][lane] + sums[1][lane]) + (sums[2][lane] + sums[3][lane]);
+            if (job.scale) s *= job.scale[i];
+            const int j = k / job.C, c = k - j * job.C;
+            store_as(job.out + (int64_t)i * per_adapter + (job.by_rank ? k : c * a.r + j), s);
         }
-        if (job.scale) s *= job.scale[i];
-        store_as(job.out + (job.by_rank ? k : ((int64_t)i * job.C + c) * a.r + j), s);
     }
 }
 
@@ -373,11 +495,17 @@ size_t up256(size_t v) { return (v + 255) & ~(size_t)255; }
 size_t rank_bytes(const ProjArgs &a) { return up256((size_t)a.rows * a.r * sizeof(float)); }
 bool narrow(const ProjArgs &a) { return a.M + a.r <= 64; }
 
-// Four waves share the summed axis while whole waves to a tile of rows would
-// leave CUs idle.  The same rule wherever rows meet A: the hidden rows then
-// have the same bits from every kernel.
+// Waves that share the summed axis of a product: four while whole waves to one
+// would leave CUs idle, sixteen for a handful.  The same rule wherever rows meet
+// A: the hidden rows then have the same bits from every kernel.
 template <typename T>
-bool share_axis(int64_t rows, int C) { return rows <= 16 * 4096 && C >= 8 * kStep<T>; }
+int axis_waves(int64_t rows, int C)
+{
+    if (rows <= 256 && C >= 32 * kStep<T>) return 16;
+    return rows <= 16 * 4096 && C >= 8 * kStep<T> ? 4 : 1;
+}
+
+bool both(const ProjArgs &a) { return a.M <= 16 && a.r <= 16; }
 
 struct RunPlan {
     int run_rows, runs;
@@ -391,7 +519,7 @@ RunPlan run_plan(const ProjArgs &a)
     const int nb = a.r <= 16 ? 1 : a.r <= 32 ? 2 : 4, ct = nb == 1 ? 256 : nb == 2 ? 128 : 64;
     const int64_t ctiles = (a.K + ct - 1) / ct + (a.M + ct - 1) / ct;
     const double part = (double)a.n * a.r * (a.K + a.M) * sizeof(float);
-    int64_t runs = std::max<int64_t>(1, std::min<int64_t>(1024 / ctiles, a.rows / 512));
+    int64_t runs = std::max<int64_t>(1, std::min<int64_t>(2048 / ctiles, a.rows / 512));
     runs = std::max<int64_t>(1, std::min<int64_t>(runs, (int64_t)(268435456.0 / part)));
     RunPlan p;
     p.run_rows = (int)(((a.rows + runs - 1) / runs + 63) / 64 * 64);
@@ -407,13 +535,16 @@ template <typename T, int NB, bool TRANS>
 hipError_t go_rank(const T *v, int64_t vs, int64_t rows, int C, const T *f, int n, int r, const float *scale,
                    const int *ids, float *t, hipStream_t s)
 {
-    const int64_t tiles = (rows + 15) / 16;
-    if (share_axis<T>(rows, C))
-        hipLaunchKernelGGL((rank_rows<T, NB, 4, TRANS>), dim3(grid_of(tiles)), dim3(256), 0, s, v, vs, rows, C, f, n, r,
-                           scale, ids, t);
-    else
-        hipLaunchKernelGGL((rank_rows<T, NB, 1, TRANS>), dim3(grid_of((tiles + 3) / 4)), dim3(256), 0, s, v, vs, rows, C,
-                           f, n, r, scale, ids, t);
+    const int waves = axis_waves<T>(rows, C);
+    // 64 sixteens of 1024 rows over the workgroups of an adapter: one each where
+    // there are few adapters, fewer workgroups where the rows spread over many
+    const int per = waves == 1 ? 4 : 1, most = (int)std::min<int64_t>(64, (rows + 15) / 16);
+    const int slots = std::max(1, std::min(most, std::max(4, 256 / n)) / per);
+    const RankArgs<T> a{v, f, vs, rows, C, n, r, slots, scale, ids, t};
+    const dim3 grid(slots, (unsigned)std::min<int64_t>((rows + 1023) / 1024 * n, 65535));
+    if (waves == 16) hipLaunchKernelGGL((rank_rows<T, NB, 16, TRANS>), grid, dim3(1024), 0, s, a);
+    else if (waves == 4) hipLaunchKernelGGL((rank_rows<T, NB, 4, TRANS>), grid, dim3(256), 0, s, a);
+    else hipLaunchKernelGGL((rank_rows<T, NB, 1, TRANS>), grid, dim3(256), 0, s, a);
     return hipGetLastError();
 }
 
@@ -431,18 +562,18 @@ template <typename T, int NB>
 hipError_t go_narrow(const ProjArgs &a, T *y, int64_t ys, float *hidden, hipStream_t s)
 {
     const int64_t tiles = (a.rows + 15) / 16;
-    if (share_axis<T>(a.rows, a.K)) {
+    const int waves = axis_waves<T>(a.rows, a.K);
+    if (waves == 16)
+        hipLaunchKernelGGL((project_narrow<T, 1, NB, 16>), dim3(grid_of(tiles)), dim3(1024), 0, s, a, y, ys, hidden);
+    else if (waves == 4)
         hipLaunchKernelGGL((project_narrow<T, 1, NB, 4>), dim3(grid_of(tiles)), dim3(256), 0, s, a, y, ys, hidden);
-    } else {
-        constexpr int RB = 2;
-        hipLaunchKernelGGL((project_narrow<T, RB, NB, 1>), dim3(grid_of((tiles + 4 * RB - 1) / (4 * RB))), dim3(256), 0, s,
-                           a, y, ys, hidden);
-    }
+    else
+        hipLaunchKernelGGL((project_narrow<T, 2, NB, 1>), dim3(grid_of((tiles + 7) / 8)), dim3(256), 0, s, a, y, ys, hidden);
     return hipGetLastError();
 }
 
 template <typename T>
-hipError_t project(const ProjArgs &a, int dtype, T *y, int64_t ys, float *hidden, float *h, hipStream_t s)
+hipError_t project(const ProjArgs &a, int dtype, T *y, int64_t ys, float *hidden, float *h, float *parts, hipStream_t s)
 {
     if (narrow(a)) {
         const int cols = a.M + a.r;
@@ -454,8 +585,16 @@ hipError_t project(const ProjArgs &a, int dtype, T *y, int64_t ys, float *hidden
         hipError_t e = rank_product<T, false>((const T *)a.x, a.xs, a.rows, a.K, (const T *)a.a, a.n, a.r, nullptr, a.ids, h, s);
         if (e != hipSuccess) return e;
     }
-    const WideArgs w{a.x, a.w, a.b, y, a.rows, a.xs, a.ws, ys, a.K, a.M, a.n, a.r, a.bias, a.scale, h, a.ids};
+    const WideArgs w{a.x, a.w, a.b, y, a.rows, a.xs, a.ws, ys, a.K, a.M, a.n, a.r, a.bias, a.scale, h, a.ids, parts};
     return launch_wide(w, dtype, false, s);
+}
+
+template <typename T>
+hipError_t join_factors(const FactorArgs<T> &a, hipStream_t s)
+{
+    const int most = a.r * std::max(a.job[0].C, a.job[1].C);
+    hipLaunchKernelGGL(factor_join<T>, dim3(grid_of((int64_t)a.n * ((most + 63) / 64)), 2), dim3(256), 0, s, a);
+    return hipGetLastError();
 }
 
 template <typename T, int NB>
@@ -464,10 +603,6 @@ hipError_t go_factor(const FactorArgs<T> &a, hipStream_t s)
     const int64_t units = (int64_t)a.n * a.runs;
     hipLaunchKernelGGL((factor_grad<T, NB>), dim3(a.job[0].ctiles + a.job[1].ctiles, (unsigned)std::min<int64_t>(units, 65535)),
                        dim3(256), 0, s, a);
-    hipError_t e = hipGetLastError();
-    if (e != hipSuccess || a.runs == 1) return e;
-    const int64_t most = (int64_t)a.n * a.r * std::max(a.job[0].C, a.job[1].C);
-    hipLaunchKernelGGL(factor_join<T>, dim3(grid_of((most + 255) / 256), 2), dim3(256), 0, s, a);
     return hipGetLastError();
 }
 
@@ -480,9 +615,13 @@ hipError_t project_grad(const ProjArgs &a, int dtype, const T *g, int64_t gs, co
     ws += rank_bytes(a);
     float *own = (float *)ws;
     ws += rank_bytes(a);
+    float *parts = (float *)ws;  // the rows' gradient and the factors' one after the other
+    const bool fused = both(a);
     if (a.n && a.rows) {
-        e = rank_product<T, true>(g, gs, a.rows, a.M, (const T *)a.b, a.n, a.r, a.scale, a.ids, u, s);
-        if (e != hipSuccess) return e;
+        if (!fused || gx) {
+            e = rank_product<T, true>(g, gs, a.rows, a.M, (const T *)a.b, a.n, a.r, a.scale, a.ids, u, s);
+            if (e != hipSuccess) return e;
+        }
         if (!h && ga) {
             e = rank_product<T, false>((const T *)a.x, a.xs, a.rows, a.K, (const T *)a.a, a.n, a.r, nullptr, a.ids, own, s);
             if (e != hipSuccess) return e;
@@ -503,12 +642,20 @@ hipError_t project_grad(const ProjArgs &a, int dtype, const T *g, int64_t gs, co
         f.r = a.r;
         f.ids = a.ids;
         f.used = p.runs > 1 ? (uint8_t *)(ws + p.parts[0] + p.parts[1]) : nullptr;
-        e = nb == 1 ? go_factor<T, 1>(f, s) : nb == 2 ? go_factor<T, 2>(f, s) : nb == 4 ? go_factor<T, 4>(f, s)
-                                                                                        : go_factor<T, 8>(f, s);
+        f.b = (const T *)a.b;
+        if (fused) {
+            hipLaunchKernelGGL(factor_both<T>, dim3(f.job[0].ctiles, (unsigned)std::min<int64_t>((int64_t)a.n * p.runs, 65535)),
+                               dim3(256), 0, s, f);
+            e = hipGetLastError();
+        } else {
+            e = nb == 1 ? go_factor<T, 1>(f, s) : nb == 2 ? go_factor<T, 2>(f, s) : nb == 4 ? go_factor<T, 4>(f, s)
+                                                                                            : go_factor<T, 8>(f, s);
+        }
+        if (e == hipSuccess && p.runs > 1) e = join_factors(f, s);
         if (e != hipSuccess) return e;
     }
     if (gx && a.rows) {
-        const WideArgs w{g, a.w, a.a, gx, a.rows, gs, a.ws, gxs, a.M, a.K, a.n, a.r, nullptr, nullptr, u, a.ids};
+        const WideArgs w{g, a.w, a.a, gx, a.rows, gs, a.ws, gxs, a.M, a.K, a.n, a.r, nullptr, nullptr, u, a.ids, parts};
         return launch_wide(w, dtype, true, s);
     }
     return hipSuccess;
@@ -516,19 +663,25 @@ hipError_t project_grad(const ProjArgs &a, int dtype, const T *g, int64_t gs, co
 
 }  // namespace
 
-size_t project_workspace(const ProjArgs &a, int) { return narrow(a) ? 0 : rank_bytes(a); }
+size_t project_workspace(const ProjArgs &a, int dtype)
+{
+    if (!a.rows || narrow(a)) return 0;
+    return rank_bytes(a) + wide_parts(a.rows, a.M, a.K, dtype);
+}
 
 hipError_t launch_project(const ProjArgs &a, int dtype, void *y, int64_t ys, float *hidden, void *ws, hipStream_t s)
 {
-    float *h = hidden ? hidden : (float *)ws;
-    return dtype == DT_BF16 ? project(a, dtype, (uint16_t *)y, ys, hidden, h, s) : project(a, dtype, (float *)y, ys, hidden, h, s);
+    float *h = hidden ? hidden : (float *)ws, *parts = (float *)((char *)ws + rank_bytes(a));
+    return dtype == DT_BF16 ? project(a, dtype, (uint16_t *)y, ys, hidden, h, parts, s)
+                            : project(a, dtype, (float *)y, ys, hidden, h, parts, s);
 }
 
-size_t project_grad_workspace(const ProjArgs &a, int)
+size_t project_grad_workspace(const ProjArgs &a, int dtype)
 {
-    if (!a.n) return 0;
+    const size_t rows = a.rows ? wide_parts(a.rows, a.K, a.M, dtype) : 0;
+    if (!a.n) return rows;
     const RunPlan p = run_plan(a);
-    return 2 * rank_bytes(a) + p.parts[0] + p.parts[1] + p.used;
+    return 2 * rank_bytes(a) + std::max(rows, p.parts[0] + p.parts[1] + p.used);
 }
 
 hipError_t launch_project_grad(const ProjArgs &a, int dtype, const void *g, int64_t gs, const float *hidden, void *gx,

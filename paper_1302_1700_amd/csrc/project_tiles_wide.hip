@@ -56,7 +56,7 @@ __device__ __forceinline__ void split_operand(const float *v, Operand<uint16_t> 
 }
 
 template <typename T, bool TRANS, int BM, int BN>
-__global__ __launch_bounds__(256, BM == 256 ? 1 : 2) void project_tiles(WideArgs a, int tiles_m, int tiles_n)
+__global__ __launch_bounds__(256, BM == 256 ? 1 : 2) void project_tiles(WideArgs a, int tiles_m, int tiles_n, int per_split)
 {
     constexpr int D = kDepth<T>, E = Operand<T>::kE;
     static_assert(D == 2 * kStep<T>, "two block products a step");
@@ -75,6 +75,8 @@ __global__ __launch_bounds__(256, BM == 256 ? 1 : 2) void project_tiles(WideArgs
         const int group = 8 * tiles_n, g0 = tile / group * 8, high = min(8, tiles_m - g0), in = tile % group;
         tile = (g0 + in % high) * tiles_n + in / high;
     }
+    // blockIdx.y's stretch of the summed axis (per_split: the whole of it)
+    const int c_begin = (int)blockIdx.y * per_split, C = min(a.C - c_begin, per_split);
     const int64_t m0 = (int64_t)(tile / tiles_n) * BM;
     const int n0 = tile % tiles_n * BN;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, q = lane & 15, g = lane >> 4;
@@ -88,7 +90,8 @@ __global__ __launch_bounds__(256, BM == 256 ? 1 : 2) void project_tiles(WideArgs
     int kb[PB];                  // TRANS: the piece's row of W
 #pragma unroll
     for (int i = 0; i < PA; ++i)
-        pa[i] = reinterpret_cast<const T *>(a.v) + clamp_row(m0 + i * 32 + (threadIdx.x >> 3), a.rows) * a.vs + (threadIdx.x & 7) * E;
+        pa[i] = reinterpret_cast<const T *>(a.v) + clamp_row(m0 + i * 32 + (threadIdx.x >> 3), a.rows) * a.vs +
+                c_begin + (threadIdx.x & 7) * E;
 #pragma unroll
     for (int i = 0; i < PB; ++i) {
         const int piece = i * 256 + threadIdx.x;
@@ -96,11 +99,11 @@ __global__ __launch_bounds__(256, BM == 256 ? 1 : 2) void project_tiles(WideArgs
             kb[i] = piece / RPB;
             int col = n0 + piece % RPB * E;
             if (a.cols % E == 0) col = min(col, a.cols - E);  // whole pieces lie inside or outside
-            pb[i] = reinterpret_cast<const T *>(a.w) + (int64_t)kb[i] * a.ws + col;
+            pb[i] = reinterpret_cast<const T *>(a.w) + (int64_t)(c_begin + kb[i]) * a.ws + col;
         } else {
             kb[i] = 0;
             pb[i] = reinterpret_cast<const T *>(a.w) + (int64_t)min(n0 + i * 32 + (int)(threadIdx.x >> 3), a.cols - 1) * a.ws +
-                    (threadIdx.x & 7) * E;
+                    c_begin + (threadIdx.x & 7) * E;
         }
     }
     const int step_b = TRANS ? 0 : D;
@@ -118,14 +121,14 @@ __global__ __launch_bounds__(256, BM == 256 ? 1 : 2) void project_tiles(WideArgs
     auto fetch_checked = [&](int step) {
         const int c0 = step * D;
 #pragma unroll
-        for (int i = 0; i < PA; ++i) ra[i] = load_operand(pa[i] + c0, a.C - c0 - (int)(threadIdx.x & 7) * E).v;
+        for (int i = 0; i < PA; ++i) ra[i] = load_operand(pa[i] + c0, C - c0 - (int)(threadIdx.x & 7) * E).v;
 #pragma unroll
         for (int i = 0; i < PB; ++i) {
             if constexpr (TRANS) {
                 const int have = a.cols % E == 0 ? E : a.cols - (n0 + (i * 256 + (int)threadIdx.x) % RPB * E);
-                rb[i] = load_operand(pb[i] + step * step_rows, c0 + kb[i] < a.C ? have : 0).v;
+                rb[i] = load_operand(pb[i] + step * step_rows, c0 + kb[i] < C ? have : 0).v;
             } else {
-                rb[i] = load_operand(pb[i] + c0, a.C - c0 - (int)(threadIdx.x & 7) * E).v;
+                rb[i] = load_operand(pb[i] + c0, C - c0 - (int)(threadIdx.x & 7) * E).v;
             }
         }
     };
@@ -183,9 +186,9 @@ __global__ __launch_bounds__(256, BM == 256 ? 1 : 2) void project_tiles(WideArgs
             for (int j = 0; j < WN; ++j) acc[i][j] = block_product(ob[j], oa[i], acc[i][j]);
     };
 
-    const int steps = (a.C + D - 1) / D;
+    const int steps = (C + D - 1) / D;
     // steps that are read without checks
-    const int whole = TRANS && a.cols % E != 0 && n0 + BN > a.cols ? 0 : a.C / D;
+    const int whole = TRANS && a.cols % E != 0 && n0 + BN > a.cols ? 0 : C / D;
     auto get = [&](int step) {
         if (step < whole) fetch(step);
         else if (step < steps) fetch_checked(step);
@@ -214,6 +217,27 @@ __global__ __launch_bounds__(256, BM == 256 ? 1 : 2) void project_tiles(WideArgs
         __syncthreads();
         if (s + 1 < steps) read((s + 1) & 1, 0, oa[0], ob[0]);
         products(oa[1], ob[1]);
+    }
+
+    if (per_split < a.C) {
+        float *part = a.parts + (int64_t)blockIdx.y * a.rows * a.cols;
+#pragma unroll
+        for (int i = 0; i < WM; ++i) {
+            const int64_t row = m0 + wm + i * 16 + q;
+            if (row >= a.rows) continue;
+#pragma unroll
+            for (int j = 0; j < WN; ++j) {
+                const int col = n0 + wn + j * 16 + g * 4;
+                float *to = part + row * a.cols + col;
+                if (col + 4 <= a.cols) store_words<16>(to, __builtin_bit_cast(Words<16>::type, acc[i][j]));
+                else {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (col + e < a.cols) to[e] = acc[i][j][e];
+                }
+            }
+        }
+        return;
     }
 
     // the adapters' part
@@ -290,8 +314,65 @@ __global__ __launch_bounds__(256, BM == 256 ? 1 : 2) void project_tiles(WideArgs
     }
 }
 
+// Joins the stretches of the summed axis in their order and adds the adapters'
+// part: a thread to four columns of a row.
+template <typename T, bool TRANS>
+__global__ __launch_bounds__(256) void project_join(WideArgs a, int splits)
+{
+    constexpr int E = Operand<T>::kE;
+    const int quads = (a.cols + 3) / 4;
+    const int64_t total = a.rows * quads;
+    for (int64_t k = (int64_t)blockIdx.x * 256 + threadIdx.x; k < total; k += (int64_t)gridDim.x * 256) {
+        const int64_t row = k / quads;
+        const int col = (int)(k - row * quads) * 4, have = min(4, a.cols - col);
+        float y[4] = {0.f, 0.f, 0.f, 0.f}, z[4] = {0.f, 0.f, 0.f, 0.f};
+        for (int s = 0; s < splits; ++s) {
+            const float *p = a.parts + (s * a.rows + row) * a.cols + col;
+            if (have == 4) {
+                float v[4];
+                unpack<float, 4>(load_words<16>(p), v);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) y[e] += v[e];
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (e < have) y[e] += p[e];
+            }
+        }
+        const int id = a.n ? a.ids[row] : -1;
+        if (id >= 0 && id < a.n) {
+            const T *f = reinterpret_cast<const T *>(a.f) + (int64_t)id * a.cols * a.r;
+            const float *t = a.t + row * a.r;
+            if constexpr (TRANS) {
+                for (int j = 0; j < a.r; ++j)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (e < have) z[e] = fmaf(t[j], to_f32(f[(int64_t)j * a.cols + col + e]), z[e]);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    if (e >= have) continue;
+                    for (int j = 0; j < a.r; j += E) {
+                        const Operand<T> o = load_operand(f + (int64_t)(col + e) * a.r + j, a.r - j);
+#pragma unroll
+                        for (int p = 0; p < E; ++p)
+                            if (j + p < a.r) z[e] = fmaf(t[j + p], to_f32((T)o.v[p]), z[e]);
+                    }
+                }
+            }
+            const float sc = !TRANS && a.scale ? a.scale[id] : 1.f;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) y[e] = fmaf(z[e], sc, y[e]);
+        }
+        T *to = reinterpret_cast<T *>(a.out) + row * a.os + col;
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (e < have) store_as(to + e, a.n && id >= a.n ? NAN : y[e] + (a.bias ? a.bias[col + e] : 0.f));
+    }
+}
+
 template <typename T, bool TRANS, int BM, int BN>
-hipError_t go(const WideArgs &a, hipStream_t s)
+hipError_t go(const WideArgs &a, int splits, int per_split, hipStream_t s)
 {
     const int64_t tm = (a.rows + BM - 1) / BM;
     const int tn = (a.cols + BN - 1) / BN;
@@ -308,29 +389,61 @@ hipError_t go(const WideArgs &a, hipStream_t s)
             p.t = a.t + row * a.r;
             p.ids = a.ids + row;
         }
-        hipLaunchKernelGGL((project_tiles<T, TRANS, BM, BN>), dim3((unsigned)(m * tn)), dim3(256), 0, s, p, (int)m, tn);
+        hipLaunchKernelGGL((project_tiles<T, TRANS, BM, BN>), dim3((unsigned)(m * tn), splits), dim3(256), 0, s,
+                           p, (int)m, tn, per_split);
         hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
     return hipSuccess;
 }
 
-template <typename T, bool TRANS>
-hipError_t choose(const WideArgs &a, hipStream_t s)
+struct WidePlan {
+    int tile, splits, per_split;
+};
+
+// 128 x 128 tiles where they give every CU one, else 64 x 64 ones; where even
+// these leave CUs idle the summed axis is split in stretches of four steps or
+// more (a launch more, and the parts' way through memory).
+WidePlan wide_plan(int64_t rows, int cols, int C, int dtype)
 {
-    const auto tiles = [&](int b) { return ((a.rows + b - 1) / b) * ((a.cols + b - 1) / b); };
-    if constexpr (sizeof(T) == 2)
-        if (tiles(256) < 0) return go<T, TRANS, 256, 256>(a, s);
-    if (tiles(128) >= 256) return go<T, TRANS, 128, 128>(a, s);
-    return go<T, TRANS, 64, 64>(a, s);
+    const auto tiles = [&](int b) { return ((rows + b - 1) / b) * ((cols + b - 1) / b); };
+    WidePlan p{64, 1, C};
+    if (tiles(128) >= 256) p.tile = 128;
+    else if (tiles(64) < 256) {
+        const int depth = dtype == DT_BF16 ? 64 : 32, steps = (C + depth - 1) / depth;
+        const int splits = (int)std::min<int64_t>((512 + tiles(64) - 1) / tiles(64), steps / 4);
+        if (splits > 1) {
+            p.per_split = (steps + splits - 1) / splits * depth;
+            p.splits = (C + p.per_split - 1) / p.per_split;
+        }
+    }
+    return p;
+}
+
+template <typename T, bool TRANS>
+hipError_t run(const WideArgs &a, int dtype, hipStream_t s)
+{
+    const WidePlan p = wide_plan(a.rows, a.cols, a.C, dtype);
+    if (p.tile == 128) return go<T, TRANS, 128, 128>(a, 1, a.C, s);
+    hipError_t e = go<T, TRANS, 64, 64>(a, p.splits, p.per_split, s);
+    if (e != hipSuccess || p.splits == 1) return e;
+    hipLaunchKernelGGL((project_join<T, TRANS>), dim3(grid_of((a.rows * ((a.cols + 3) / 4) + 255) / 256)), dim3(256), 0, s, a,
+                       p.splits);
+    return hipGetLastError();
 }
 
 }  // namespace
 
+size_t wide_parts(int64_t rows, int cols, int C, int dtype)
+{
+    const WidePlan p = wide_plan(rows, cols, C, dtype);
+    return p.splits > 1 ? (size_t)p.splits * rows * cols * sizeof(float) : 0;
+}
+
 hipError_t launch_wide(const WideArgs &a, int dtype, bool trans, hipStream_t s)
 {
-    if (dtype == DT_BF16) return trans ? choose<uint16_t, true>(a, s) : choose<uint16_t, false>(a, s);
-    return trans ? choose<float, true>(a, s) : choose<float, false>(a, s);
+    if (dtype == DT_BF16) return trans ? run<uint16_t, true>(a, dtype, s) : run<uint16_t, false>(a, dtype, s);
+    return trans ? run<float, true>(a, dtype, s) : run<float, false>(a, dtype, s);
 }
 
 }  // namespace fs

@@ -105,17 +105,17 @@ def test_no_rows_are_no_work():
 
 
 def _proj(**kw):
-    d = dict(rows=4, k=6, m=5, dtype=0, n_adapters=2, rank=3, d_x=BAD, x_stride=6, d_w=BAD, w_stride=6, d_bias=BAD,
+    d = dict(rows=4, k=6, m=70, dtype=0, n_adapters=2, rank=3, d_x=BAD, x_stride=6, d_w=BAD, w_stride=6, d_bias=BAD,
              d_a=BAD, d_b=BAD, d_scale=BAD, d_ids=BAD)
     d.update(kw)
     return fsb.fs_projection(**d)
 
 
-def _project(lib, y=BAD, y_stride=5, hidden=None, ws=BAD, have=1 << 40, **kw):
+def _project(lib, y=BAD, y_stride=70, hidden=None, ws=BAD, have=1 << 40, **kw):
     return lib.fs_project(ctypes.byref(_proj(**kw)), y, y_stride, hidden, ws, have, None)
 
 
-def _project_grad(lib, g=BAD, g_stride=5, hidden=None, gx=BAD, gx_stride=6, ga=BAD, gb=BAD, ws=BAD, have=1 << 40, **kw):
+def _project_grad(lib, g=BAD, g_stride=70, hidden=None, gx=BAD, gx_stride=6, ga=BAD, gb=BAD, ws=BAD, have=1 << 40, **kw):
     return lib.fs_project_grad(ctypes.byref(_proj(**kw)), g, g_stride, hidden, gx, gx_stride, ga, gb, ws, have, None)
 
 
@@ -131,7 +131,7 @@ PROJ = [(dict(rows=-1), INVALID), (dict(rows=1 << 31), UNSUPPORTED), (dict(k=0),
 
 
 @pytest.mark.parametrize("kw,status", PROJ + [
-    (dict(y=None), INVALID), (dict(y_stride=4), INVALID), (dict(y=BAD + 2), INVALID),
+    (dict(y=None), INVALID), (dict(y_stride=69), INVALID), (dict(y=BAD + 2), INVALID),
     (dict(have=0), WORKSPACE), (dict(ws=None), INVALID), (dict(ws=BAD + 16), INVALID),
     (dict(n_adapters=0, rank=0, d_a=None, d_b=None, d_scale=None, d_ids=None, hidden=BAD), INVALID)])
 def test_project_refuses(kw, status):
