@@ -55,8 +55,8 @@ __device__ __forceinline__ void row_products(const T *const (&row)[RB], const T 
 // The rows of one adapter among 1024: their offsets from the first, in order, in
 // `list`; returns how many.  All threads of the workgroup take part (NW waves);
 // `id` is called with every row's adapter once: id(row, adapter).
-template <int NW, typename Each>
-__device__ __forceinline__ int list_rows(const int *ids, int64_t at, int64_t end, int adapter, int *list, int *count,
+template <int NW, typename Id, typename Each>
+__device__ __forceinline__ int list_rows(const Id *ids, int64_t at, int64_t end, int adapter, int *list, int *count,
                                          Each each)
 {
     constexpr int G = 16 / NW > 0 ? 16 / NW : 1;  // groups of 64 ids a wave looks at
@@ -276,208 +276,192 @@ struct FactorArgs {
     int run_rows, runs, n, r;
     const int *ids;
     uint8_t *used;  // [n][runs]: the run holds rows of the adapter
-    const T *b;     // factor_both: [n][M][r]
+    const T *b;     // both in one pass: [n][M][r]
 };
 
-// Columns of a workgroup: 64 accumulators' worth, 16 ranks a block.
-template <int NB>
-constexpr int kFactorCols = NB == 1 ? 256 : NB == 2 ? 128 : 64;
-
-// Four adjacent values of a row from column c on, 0 past its C columns.
-template <typename T>
-__device__ __forceinline__ void four(const T *v, int c, int C, float (&vv)[4])
+// Four adjacent values of a row from column c on, 0 past its C columns.  QUADS
+// (C a multiple of four): always one load, from inside the row, without a
+// branch that would keep the next row's load waiting.
+template <bool QUADS, typename T>
+__device__ __forceinline__ void four(const T *v, int c, int C, bool have, float (&vv)[4])
 {
-    if (c + 4 <= C) unpack<T, 4>(load_words<4 * sizeof(T)>(v + c), vv);
-    else {
+    if (QUADS || c + 4 <= C) {
+        unpack<T, 4>(load_words<4 * sizeof(T)>(v + min(c, C - 4)), vv);
+        have &= c < C;
+    } else {
 #pragma unroll
         for (int e = 0; e < 4; ++e) vv[e] = c + e < C ? to_f32(v[c + e]) : 0.f;
     }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) vv[e] = have ? vv[e] : 0.f;
 }
 
-// Where a sum goes: the part of a run, or the gradient itself when there is one run.
+// Where sums go: the part of a run, or the gradient itself when there is one
+// run; four adjacent columns of rank j.
 template <typename T>
-__device__ __forceinline__ void store_sum(const FactorArgs<T> &a, const FactorJob<T> &job, int64_t unit, int i, int j, int c,
-                                          float s)
+__device__ __forceinline__ void store_sums(const FactorArgs<T> &a, const FactorJob<T> &job, int64_t unit, int i, int j, int c,
+                                           f4 s)
 {
-    if (j >= a.r || c >= job.C) return;
-    if (a.runs > 1) job.parts[(unit * a.r + j) * job.C + c] = s;
-    else
-        store_as(job.out + (job.by_rank ? ((int64_t)i * a.r + j) * job.C + c : ((int64_t)i * job.C + c) * a.r + j),
-                 job.scale ? s * job.scale[i] : s);
-}
-
-// Joins the four waves' blocks and stores them; element e of lane l: rank
-// 16 j + 4 (l / 16) + e, column `c` of l % 16.
-template <typename T, int NB, typename Column>
-__device__ __forceinline__ void store_blocks(const FactorArgs<T> &a, const FactorJob<T> &job, int64_t unit, int i,
-                                             const f4 (&acc)[NB], float (*sums)[64][NB * 4 + 1], Column column)
-{
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    __syncthreads();
+    if (j >= a.r) return;
+    if (a.runs > 1 && c + 4 <= job.C) {
+        store_words<16>(job.parts + (unit * a.r + j) * job.C + c, __builtin_bit_cast(Words<16>::type, s));
+        return;
+    }
 #pragma unroll
-    for (int j = 0; j < NB; ++j)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) sums[wave][lane][j * 4 + e] = acc[j][e];
-    __syncthreads();
-    for (int k = threadIdx.x; k < 64 * NB * 4; k += 256) {
-        const int l = k & 63, je = k >> 6;
-        const float s = (sums[0][l][je] + sums[1][l][je]) + (sums[2][l][je] + sums[3][l][je]);
-        store_sum(a, job, unit, i, je / 4 * 16 + (l >> 4) * 4 + je % 4, column(l & 15), s);
+    for (int e = 0; e < 4; ++e) {
+        if (c + e >= job.C) return;
+        if (a.runs > 1) job.parts[(unit * a.r + j) * job.C + c + e] = s[e];
+        else
+            store_as(job.out + (job.by_rank ? ((int64_t)i * a.r + j) * job.C + c + e : ((int64_t)i * job.C + c + e) * a.r + j),
+                     job.scale ? s[e] * job.scale[i] : s[e]);
     }
 }
 
-// Workgroup: one adapter, one run of rows, one tile of columns.  The run's rows
-// that name the adapter are listed in LDS, 1024 ids at a time; the four waves
-// take kGroups times four listed rows each in turn as the summed axis of
-// float32 products (bf16 values are exact in them).
-constexpr int kGroups = 2;
+// Workgroup: one adapter, one run of rows, 64 WC columns.  The run's rows that
+// name the adapter are listed in LDS, 1024 ids at a time, and are the summed
+// axis of float32 products (bf16 values are exact in them), four at a time, a
+// wave's loads of 4 kGroups rows in flight together.  WC waves take 64 columns
+// each, so that no sum crosses waves; where there are fewer columns, 4 / WC
+// waves share the rows and their sums are joined in LDS.  Two jobs (both
+// factors) by blockIdx.x; FUSED (M and r up to 16; MB: M's bound) makes both in
+// one pass over the rows: lane q holds column q of its adapter's B and makes
+// u = B^T g of its row from the row's 16 lanes, so u never goes through memory.
+template <int NB>
+constexpr int kGroups = NB == 1 ? 8 : NB == 2 ? 4 : 2;
 
-template <typename T, int NB>
+template <typename T, int NB, int WC, bool QUADS, int MB>
 __global__ __launch_bounds__(256) void factor_grad(FactorArgs<T> a)
 {
-    constexpr int CT = kFactorCols<NB>, CB = CT / 64;
+    constexpr bool FUSED = MB > 0;
+    constexpr int G = kGroups<NB>, WR = 4 / WC;
     __shared__ int list[1024], count[16];
-    __shared__ float sums[4][64][NB * 4 + 1];
+    __shared__ float sums[WR > 1 ? 4 : 1][WR > 1 ? (4 * NB + 1) * 4 : 1][64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, q = lane & 15, g = lane >> 4;
-    const int which = blockIdx.x >= (unsigned)a.job[0].ctiles;
-    const FactorJob<T> &job = a.job[which];
-    const int c0 = ((int)blockIdx.x - (which ? a.job[0].ctiles : 0)) * CT;
-    const int r = a.r;
+    const int which = !FUSED && blockIdx.x >= (unsigned)a.job[0].ctiles;
+    const FactorJob<T> &job = a.job[which], &jb = a.job[1];
+    const int c0 = ((int)blockIdx.x - (which ? a.job[0].ctiles : 0)) * 64 * WC + wave % WC * 64, wr = wave / WC;
+    const int r = a.r, M = jb.C, C = job.C;
+    const bool second = FUSED && blockIdx.x == 0 && wave % WC == 0;  // this wave also makes the other factor's
     for (int64_t unit = blockIdx.y; unit < (int64_t)a.n * a.runs; unit += gridDim.y) {
         const int i = (int)(unit / a.runs), run = (int)(unit - (int64_t)i * a.runs);
         const int64_t begin = (int64_t)run * a.run_rows, end = std::min(a.rows, begin + a.run_rows);
-        f4 acc[CB * 4][NB];
+        float bi[FUSED ? MB : 1];
+        if constexpr (FUSED) {
+            const float sc = jb.scale ? jb.scale[i] : 1.f;
 #pragma unroll
-        for (int b = 0; b < CB * 4; ++b)
-#pragma unroll
-            for (int j = 0; j < NB; ++j) acc[b][j] = f4{0.f, 0.f, 0.f, 0.f};
-        bool seen = false;
-        for (int64_t at = begin; at < end; at += 1024) {
-            const int total = list_rows<4>(a.ids, at, end, i, list, count, [](int64_t, int) {});
-            seen |= total > 0;
-            for (int l = wave * 4 * kGroups; l < total; l += 16 * kGroups) {
-                float tv[kGroups][NB], vv[kGroups][CB][4];
-#pragma unroll
-                for (int k = 0; k < kGroups; ++k) {
-                    const bool have = l + k * 4 + g < total;
-                    const int64_t row = at + list[have ? l + k * 4 + g : l];
-#pragma unroll
-                    for (int j = 0; j < NB; ++j)
-                        tv[k][j] = have && j * 16 + q < r ? job.t[row * r + j * 16 + q] : 0.f;
-#pragma unroll
-                    for (int b = 0; b < CB; ++b) {
-                        four(job.v + row * job.vs, c0 + b * 64 + q * 4, job.C, vv[k][b]);
-                        if (!have) vv[k][b][0] = vv[k][b][1] = vv[k][b][2] = vv[k][b][3] = 0.f;
-                    }
-                }
-#pragma unroll
-                for (int k = 0; k < kGroups; ++k)
-#pragma unroll
-                    for (int b = 0; b < CB; ++b)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e)
-#pragma unroll
-                            for (int j = 0; j < NB; ++j)
-                                acc[b * 4 + e][j] =
-                                    __builtin_amdgcn_mfma_f32_16x16x4f32(tv[k][j], vv[k][b][e], acc[b * 4 + e][j], 0, 0, 0);
-            }
+            for (int m = 0; m < MB; ++m) bi[m] = m < M && q < r ? to_f32(a.b[((int64_t)i * M + m) * r + q]) * sc : 0.f;
         }
-        if (threadIdx.x == 0 && blockIdx.x == 0 && a.used) a.used[unit] = seen;
-        if (!seen && a.runs > 1) continue;
+        f4 acc[4][NB], gb = f4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int bp = 0; bp < CB * 4; ++bp)
-            store_blocks<T, NB>(a, job, unit, i, acc[bp], sums,
-                                [&](int l) { return c0 + (bp >> 2) * 64 + l * 4 + (bp & 3); });
-    }
-}
-
-// Few outputs and ranks (M and r up to 16): both factors' gradients in one pass
-// over the rows.  A lane holds column q of its adapter's B and makes u = B^T g
-// of its row from the row's 16 lanes, so u never goes through memory.
-template <typename T>
-__global__ __launch_bounds__(256) void factor_both(FactorArgs<T> a)
-{
-    constexpr int CB = 4;
-    __shared__ int list[1024], count[16];
-    __shared__ float sums[4][64][5];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, q = lane & 15, g = lane >> 4;
-    const FactorJob<T> &ja = a.job[0], &jb = a.job[1];
-    const int c0 = (int)blockIdx.x * 256, r = a.r, M = jb.C;
-    for (int64_t unit = blockIdx.y; unit < (int64_t)a.n * a.runs; unit += gridDim.y) {
-        const int i = (int)(unit / a.runs), run = (int)(unit - (int64_t)i * a.runs);
-        const int64_t begin = (int64_t)run * a.run_rows, end = std::min(a.rows, begin + a.run_rows);
-        const float sc = jb.scale ? jb.scale[i] : 1.f;
-        float bi[16];
+        for (int p = 0; p < 4; ++p)
 #pragma unroll
-        for (int m = 0; m < 16; ++m) bi[m] = m < M && q < r ? to_f32(a.b[((int64_t)i * M + m) * r + q]) * sc : 0.f;
-        f4 acc[CB * 4], gb = f4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int b = 0; b < CB * 4; ++b) acc[b] = f4{0.f, 0.f, 0.f, 0.f};
+            for (int j = 0; j < NB; ++j) acc[p][j] = f4{0.f, 0.f, 0.f, 0.f};
         bool seen = false;
         for (int64_t at = begin; at < end; at += 1024) {
             const int total = list_rows<4>(a.ids, at, end, i, list, count, [](int64_t, int) {});
             seen |= total > 0;
-            for (int l = wave * 4 * kGroups; l < total; l += 16 * kGroups) {
-                float hv[kGroups], gv[kGroups], vv[kGroups][CB][4];
+            if (c0 >= C && !second) continue;
+            for (int l = wr * 4 * G; l < total; l += WR * 4 * G) {
+                float tv[G][NB], vv[G][4], gv[FUSED ? G : 1];
 #pragma unroll
-                for (int k = 0; k < kGroups; ++k) {
+                for (int k = 0; k < G; ++k) {
                     const bool have = l + k * 4 + g < total;
                     const int64_t row = at + list[have ? l + k * 4 + g : l];
-                    gv[k] = have && q < M ? to_f32(jb.v[row * jb.vs + q]) : 0.f;
-                    hv[k] = have && q < r ? jb.t[row * r + q] : 0.f;
 #pragma unroll
-                    for (int b = 0; b < CB; ++b) {
-                        four(ja.v + row * ja.vs, c0 + b * 64 + q * 4, ja.C, vv[k][b]);
-                        if (!have) vv[k][b][0] = vv[k][b][1] = vv[k][b][2] = vv[k][b][3] = 0.f;
+                    for (int j = 0; j < NB; ++j) {
+                        const float *t = FUSED ? jb.t : job.t;
+                        tv[k][j] = t[row * r + std::min(j * 16 + q, r - 1)];
+                        tv[k][j] = have && j * 16 + q < r ? tv[k][j] : 0.f;
                     }
+                    if constexpr (FUSED) {
+                        gv[k] = to_f32(jb.v[row * jb.vs + std::min(q, M - 1)]);
+                        gv[k] = have && q < M ? gv[k] : 0.f;
+                    }
+                    four<QUADS>(job.v + row * job.vs, c0 + q * 4, C, have, vv[k]);
                 }
 #pragma unroll
-                for (int k = 0; k < kGroups; ++k) {
-                    float u = 0.f;
+                for (int k = 0; k < G; ++k) {
+                    if constexpr (FUSED) {
+                        if (second) gb = __builtin_amdgcn_mfma_f32_16x16x4f32(tv[k][0], gv[k], gb, 0, 0, 0);
+                        float u = 0.f;
 #pragma unroll
-                    for (int m = 0; m < 16; ++m)
-                        if (m < M) u = fmaf(__shfl(gv[k], (lane & 48) + m), bi[m], u);
-                    gb = __builtin_amdgcn_mfma_f32_16x16x4f32(hv[k], gv[k], gb, 0, 0, 0);
+                        for (int m = 0; m < MB; ++m) u = fmaf(__shfl(gv[k], (lane & 48) + m), bi[m], u);
+                        tv[k][0] = u;
+                    }
 #pragma unroll
-                    for (int b = 0; b < CB; ++b)
+                    for (int p = 0; p < 4; ++p)
 #pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            acc[b * 4 + e] = __builtin_amdgcn_mfma_f32_16x16x4f32(u, vv[k][b][e], acc[b * 4 + e], 0, 0, 0);
+                        for (int j = 0; j < NB; ++j)
+                            acc[p][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(tv[k][j], vv[k][p], acc[p][j], 0, 0, 0);
                 }
             }
         }
         if (threadIdx.x == 0 && blockIdx.x == 0 && a.used) a.used[unit] = seen;
         if (!seen && a.runs > 1) continue;
+        if constexpr (WR > 1) {
+            __syncthreads();
 #pragma unroll
-        for (int bp = 0; bp < CB * 4; ++bp) {
-            const f4 one[1] = {acc[bp]};
-            store_blocks<T, 1>(a, ja, unit, i, one, sums, [&](int l) { return c0 + (bp >> 2) * 64 + l * 4 + (bp & 3); });
+            for (int e = 0; e < 4; ++e) {
+#pragma unroll
+                for (int j = 0; j < NB; ++j)
+#pragma unroll
+                    for (int p = 0; p < 4; ++p) sums[wave][(j * 4 + p) * 4 + e][lane] = acc[p][j][e];
+                sums[wave][NB * 16 + e][lane] = gb[e];
+            }
+            __syncthreads();
+            if (wr == 0) {
+#pragma unroll
+                for (int o = 1; o < WR; ++o)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+#pragma unroll
+                        for (int j = 0; j < NB; ++j)
+#pragma unroll
+                            for (int p = 0; p < 4; ++p) acc[p][j][e] += sums[o * WC + wave][(j * 4 + p) * 4 + e][lane];
+                        gb[e] += sums[o * WC + wave][NB * 16 + e][lane];
+                    }
+            }
+            if (wr != 0) continue;
         }
-        if (blockIdx.x == 0) {
-            const f4 one[1] = {gb};
-            store_blocks<T, 1>(a, jb, unit, i, one, sums, [&](int l) { return l; });
+        // element e of lane l: rank 16 j + 4 g + e; block p: column c0 + 4 q + p
+#pragma unroll
+        for (int j = 0; j < NB; ++j)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                store_sums(a, job, unit, i, j * 16 + g * 4 + e, c0 + q * 4,
+                           f4{acc[0][j][e], acc[1][j][e], acc[2][j][e], acc[3][j][e]});
+        if (second && q < M) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int j = g * 4 + e;
+                if (j >= r) continue;
+                if (a.runs > 1) jb.parts[(unit * r + j) * M + q] = gb[e];
+                else store_as(jb.out + ((int64_t)i * M + q) * r + j, jb.scale ? gb[e] * jb.scale[i] : gb[e]);
+            }
         }
     }
 }
 
-// Sums the runs' parts: 64 values to a workgroup, each wave a quarter of the
-// runs in their order, the quarters joined in order.
+// Sums the parts of the runs that hold rows of the adapter: 64 values to a
+// workgroup, each wave a quarter of these runs in their order, the quarters
+// joined in order.
 template <typename T>
 __global__ __launch_bounds__(256) void factor_join(FactorArgs<T> a)
 {
     __shared__ float sums[4][64];
+    __shared__ int list[1024], count[16];
     const FactorJob<T> &job = a.job[blockIdx.y];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int per_adapter = a.r * job.C, blocks = (per_adapter + 63) / 64;
-    const int quarter = (a.runs + 3) / 4, from = wave * quarter, to = std::min(a.runs, from + quarter);
     for (int64_t unit = blockIdx.x; unit < (int64_t)a.n * blocks; unit += gridDim.x) {
         const int i = (int)(unit / blocks), k = (int)(unit - (int64_t)i * blocks) * 64 + lane;
-        const uint8_t *used = a.used + (int64_t)i * a.runs;
-        const float *parts = job.parts + (int64_t)i * a.runs * per_adapter;
+        const float *parts = job.parts + (int64_t)i * a.runs * per_adapter + std::min(k, per_adapter - 1);
         float s = 0.f;
-        if (k < per_adapter)
-            for (int run = from; run < to; ++run)
-                if (used[run]) s += parts[(int64_t)run * per_adapter + k];
+        for (int at = 0; at < a.runs; at += 1024) {
+            const int total = list_rows<4>(a.used + (int64_t)i * a.runs, at, a.runs, 1, list, count, [](int64_t, int) {});
+            const int quarter = (total + 3) / 4, to = std::min(total, (wave + 1) * quarter);
+            for (int l = wave * quarter; l < to; ++l) s += parts[(int64_t)(at + list[l]) * per_adapter];
+        }
         __syncthreads();
         sums[wave][lane] = s;
         __syncthreads();
@@ -516,10 +500,9 @@ struct RunPlan {
 // together (then one in n of them works), parts of at most 256 MB.
 RunPlan run_plan(const ProjArgs &a)
 {
-    const int nb = a.r <= 16 ? 1 : a.r <= 32 ? 2 : 4, ct = nb == 1 ? 256 : nb == 2 ? 128 : 64;
-    const int64_t ctiles = (a.K + ct - 1) / ct + (a.M + ct - 1) / ct;
+    const int64_t ctiles = both(a) ? (a.K + 255) / 256 : (a.K + 255) / 256 + (a.M + 255) / 256;
     const double part = (double)a.n * a.r * (a.K + a.M) * sizeof(float);
-    int64_t runs = std::max<int64_t>(1, std::min<int64_t>(2048 / ctiles, a.rows / 512));
+    int64_t runs = std::max<int64_t>(1, std::min<int64_t>(2048 / ctiles, a.rows / 256));
     runs = std::max<int64_t>(1, std::min<int64_t>(runs, (int64_t)(268435456.0 / part)));
     RunPlan p;
     p.run_rows = (int)(((a.rows + runs - 1) / runs + 63) / 64 * 64);
@@ -539,7 +522,7 @@ hipError_t go_rank(const T *v, int64_t vs, int64_t rows, int C, const T *f, int 
     // 64 sixteens of 1024 rows over the workgroups of an adapter: one each where
     // there are few adapters, fewer workgroups where the rows spread over many
     const int per = waves == 1 ? 4 : 1, most = (int)std::min<int64_t>(64, (rows + 15) / 16);
-    const int slots = std::max(1, std::min(most, std::max(4, 256 / n)) / per);
+    const int slots = std::max(1, std::min(most, std::max(4, 512 / n)) / per);
     const RankArgs<T> a{v, f, vs, rows, C, n, r, slots, scale, ids, t};
     const dim3 grid(slots, (unsigned)std::min<int64_t>((rows + 1023) / 1024 * n, 65535));
     if (waves == 16) hipLaunchKernelGGL((rank_rows<T, NB, 16, TRANS>), grid, dim3(1024), 0, s, a);
@@ -597,13 +580,23 @@ hipError_t join_factors(const FactorArgs<T> &a, hipStream_t s)
     return hipGetLastError();
 }
 
-template <typename T, int NB>
-hipError_t go_factor(const FactorArgs<T> &a, hipStream_t s)
+template <typename T, int NB, int WC, int MB>
+hipError_t go_factor(FactorArgs<T> &a, hipStream_t s)
 {
-    const int64_t units = (int64_t)a.n * a.runs;
-    hipLaunchKernelGGL((factor_grad<T, NB>), dim3(a.job[0].ctiles + a.job[1].ctiles, (unsigned)std::min<int64_t>(units, 65535)),
-                       dim3(256), 0, s, a);
+    for (FactorJob<T> &j : a.job) j.ctiles = (j.C + 64 * WC - 1) / (64 * WC);
+    const dim3 grid(a.job[0].ctiles + (MB ? 0 : a.job[1].ctiles), (unsigned)std::min<int64_t>((int64_t)a.n * a.runs, 65535));
+    if (a.job[0].C % 4 == 0 && (MB || a.job[1].C % 4 == 0))
+        hipLaunchKernelGGL((factor_grad<T, NB, WC, true, MB>), grid, dim3(256), 0, s, a);
+    else
+        hipLaunchKernelGGL((factor_grad<T, NB, WC, false, MB>), grid, dim3(256), 0, s, a);
     return hipGetLastError();
+}
+
+template <typename T, int NB, int MB>
+hipError_t go_factor(FactorArgs<T> &a, hipStream_t s)
+{
+    const int C = MB ? a.job[0].C : std::max(a.job[0].C, a.job[1].C);
+    return C <= 64 ? go_factor<T, NB, 1, MB>(a, s) : C <= 128 ? go_factor<T, NB, 2, MB>(a, s) : go_factor<T, NB, 4, MB>(a, s);
 }
 
 template <typename T>
@@ -630,11 +623,9 @@ hipError_t project_grad(const ProjArgs &a, int dtype, const T *g, int64_t gs, co
     }
     if (ga) {
         const RunPlan p = run_plan(a);
-        const int nb = a.r <= 16 ? 1 : a.r <= 32 ? 2 : a.r <= 64 ? 4 : 8;
-        const int ct = nb == 1 ? 256 : nb == 2 ? 128 : 64;
         FactorArgs<T> f{};
-        f.job[0] = FactorJob<T>{u, (const T *)a.x, a.xs, a.K, 1, (a.K + ct - 1) / ct, nullptr, ga, (float *)ws};
-        f.job[1] = FactorJob<T>{h, g, gs, a.M, 0, (a.M + ct - 1) / ct, a.scale, gb, (float *)(ws + p.parts[0])};
+        f.job[0] = FactorJob<T>{u, (const T *)a.x, a.xs, a.K, 1, 0, nullptr, ga, (float *)ws};
+        f.job[1] = FactorJob<T>{h, g, gs, a.M, 0, 0, a.scale, gb, (float *)(ws + p.parts[0])};
         f.rows = a.rows;
         f.run_rows = p.run_rows;
         f.runs = p.runs;
@@ -643,14 +634,11 @@ hipError_t project_grad(const ProjArgs &a, int dtype, const T *g, int64_t gs, co
         f.ids = a.ids;
         f.used = p.runs > 1 ? (uint8_t *)(ws + p.parts[0] + p.parts[1]) : nullptr;
         f.b = (const T *)a.b;
-        if (fused) {
-            hipLaunchKernelGGL(factor_both<T>, dim3(f.job[0].ctiles, (unsigned)std::min<int64_t>((int64_t)a.n * p.runs, 65535)),
-                               dim3(256), 0, s, f);
-            e = hipGetLastError();
-        } else {
-            e = nb == 1 ? go_factor<T, 1>(f, s) : nb == 2 ? go_factor<T, 2>(f, s) : nb == 4 ? go_factor<T, 4>(f, s)
-                                                                                            : go_factor<T, 8>(f, s);
-        }
+        if (fused) e = a.M <= 4 ? go_factor<T, 1, 4>(f, s) : go_factor<T, 1, 16>(f, s);
+        else if (a.r <= 16) e = go_factor<T, 1, 0>(f, s);
+        else if (a.r <= 32) e = go_factor<T, 2, 0>(f, s);
+        else if (a.r <= 64) e = go_factor<T, 4, 0>(f, s);
+        else e = go_factor<T, 8, 0>(f, s);
         if (e == hipSuccess && p.runs > 1) e = join_factors(f, s);
         if (e != hipSuccess) return e;
     }
