@@ -55,13 +55,16 @@ __device__ __forceinline__ void split_operand(const float *v, Operand<uint16_t> 
     }
 }
 
-template <typename T, bool TRANS, int BM, int BN>
-__global__ __launch_bounds__(256, BM == 256 ? 1 : 2) void project_tiles(WideArgs a, int tiles_m, int tiles_n, int per_split)
+// WR x WC waves; two of them to a SIMD, 256 registers each.
+template <typename T, bool TRANS, int BM, int BN, int WR, int WC>
+__global__ __launch_bounds__(64 * WR * WC, 2) void project_tiles(WideArgs a, int tiles_m, int tiles_n, int per_split)
 {
     constexpr int D = kDepth<T>, E = Operand<T>::kE;
     static_assert(D == 2 * kStep<T>, "two block products a step");
-    constexpr int WM = BM / 32, WN = BN / 32;                // 16 x 16 blocks of a wave
-    constexpr int PA = BM / 32, PB = BN / 32;                // 16-byte pieces a thread stages
+    constexpr int NT = 64 * WR * WC, RT = NT / 8;            // threads, rows staged at once
+    constexpr int WM = BM / 16 / WR, WN = BN / 16 / WC;      // 16 x 16 blocks of a wave
+    constexpr int PA = BM / RT, PB = BN / RT;                // 16-byte pieces a thread stages
+    constexpr bool AHEAD = WM * WN <= 16;                    // registers for both halves' operands
     constexpr int BP = TRANS ? BN + (sizeof(T) == 2 ? 16 : 4) : 0;  // pitch of W's tile in the order of memory
     constexpr int A_BYTES = BM * 128, B_BYTES = TRANS ? D * BP * (int)sizeof(T) : BN * 128;
     __shared__ __align__(16) char lds[2 * (A_BYTES + B_BYTES)];
@@ -80,68 +83,95 @@ __global__ __launch_bounds__(256, BM == 256 ? 1 : 2) void project_tiles(WideArgs
     const int64_t m0 = (int64_t)(tile / tiles_n) * BM;
     const int n0 = tile % tiles_n * BN;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, q = lane & 15, g = lane >> 4;
-    const int wm = (wave >> 1) * (BM / 2), wn = (wave & 1) * (BN / 2);
+    const int wm = wave / WC * (BM / WR), wn = wave % WC * (BN / WC);
 
     // What the thread stages: pieces of rows (a row's eight pieces by eight
     // threads), or of W's rows of BN columns; a row or column past the end is
     // the last one, its products are not stored.
     constexpr int RPB = BN / E;  // pieces of a row of W as in memory
-    const T *pa[PA], *pb[PB];
-    int kb[PB];                  // TRANS: the piece's row of W
+    const T *va = reinterpret_cast<const T *>(a.v) + m0 * a.vs + c_begin;
+    const T *wb = reinterpret_cast<const T *>(a.w) + (TRANS ? (int64_t)c_begin * a.ws + n0 : (int64_t)n0 * a.ws + c_begin);
+    uint32_t pa[PA], pb[PB];  // a thread's places from there, in bytes
 #pragma unroll
     for (int i = 0; i < PA; ++i)
-        pa[i] = reinterpret_cast<const T *>(a.v) + clamp_row(m0 + i * 32 + (threadIdx.x >> 3), a.rows) * a.vs +
-                c_begin + (threadIdx.x & 7) * E;
+        pa[i] = (uint32_t)(((clamp_row(m0 + i * RT + (threadIdx.x >> 3), a.rows) - m0) * a.vs + (threadIdx.x & 7) * E) * sizeof(T));
 #pragma unroll
     for (int i = 0; i < PB; ++i) {
-        const int piece = i * 256 + threadIdx.x;
+        const int piece = i * NT + threadIdx.x;
         if constexpr (TRANS) {
-            kb[i] = piece / RPB;
-            int col = n0 + piece % RPB * E;
-            if (a.cols % E == 0) col = min(col, a.cols - E);  // whole pieces lie inside or outside
-            pb[i] = reinterpret_cast<const T *>(a.w) + (int64_t)(c_begin + kb[i]) * a.ws + col;
+            int col = piece % RPB * E;
+            if (a.cols % E == 0) col = min(n0 + col, a.cols - E) - n0;  // whole pieces lie inside or outside
+            pb[i] = (uint32_t)((piece / RPB * a.ws + col) * sizeof(T));
         } else {
-            kb[i] = 0;
-            pb[i] = reinterpret_cast<const T *>(a.w) + (int64_t)min(n0 + i * 32 + (int)(threadIdx.x >> 3), a.cols - 1) * a.ws +
-                    c_begin + (threadIdx.x & 7) * E;
+            pb[i] = (uint32_t)(((min(n0 + i * RT + (int)(threadIdx.x >> 3), a.cols - 1) - n0) * a.ws + (threadIdx.x & 7) * E) *
+                               sizeof(T));
         }
     }
-    const int step_b = TRANS ? 0 : D;
-    const int64_t step_rows = TRANS ? (int64_t)D * a.ws : 0;
+    const auto place = [](const T *base, uint32_t bytes) {
+        return reinterpret_cast<const T *>(reinterpret_cast<const char *>(base) + bytes);
+    };
+    // steps are fetched in their order: the bases move along
     typedef decltype(Operand<T>::v) Piece;  // 16 bytes
     Piece ra[PA], rb[PB];
-    auto fetch = [&](int step) {
+    auto advance = [&]() {
+        va += D;
+        wb += TRANS ? D * a.ws : D;
+    };
+    // Large tiles: buffer loads, whose addresses are one register a piece and a
+    // scalar that moves along (as pointers they took two each and spilled).
+    // The host sends only 16-byte aligned rows of less than 2^31 bytes a tile, and
+    // whole steps.
+    constexpr bool BUFFER = !AHEAD;
+    const __amdgpu_buffer_rsrc_t buf_a = __builtin_amdgcn_make_buffer_rsrc((void *)va, 0, 0x7fffffff, 0x00020000);
+    const __amdgpu_buffer_rsrc_t buf_b = __builtin_amdgcn_make_buffer_rsrc((void *)wb, 0, 0x7fffffff, 0x00020000);
+    int move_a = 0, move_b = 0;
+    auto fetch = [&]() {
+        if constexpr (BUFFER) {
 #pragma unroll
-        for (int i = 0; i < PA; ++i) ra[i] = __builtin_bit_cast(Piece, load_words<16>(pa[i] + (int64_t)step * D));
+            for (int i = 0; i < PA; ++i)
+                ra[i] = __builtin_bit_cast(Piece, __builtin_amdgcn_raw_buffer_load_b128(buf_a, pa[i], move_a, 0));
 #pragma unroll
-        for (int i = 0; i < PB; ++i)
-            rb[i] = __builtin_bit_cast(Piece, load_words<16>(pb[i] + (int64_t)step * step_b + step * step_rows));
+            for (int i = 0; i < PB; ++i)
+                rb[i] = __builtin_bit_cast(Piece, __builtin_amdgcn_raw_buffer_load_b128(buf_b, pb[i], move_b, 0));
+            // past the last step the last one again: nobody reads it
+            const bool more = move_a + 128 < C * (int)sizeof(T);
+            move_a += more ? 128 : 0;
+            move_b += more ? (TRANS ? D * (int)a.ws * (int)sizeof(T) : 128) : 0;
+        } else {
+#pragma unroll
+            for (int i = 0; i < PA; ++i) ra[i] = __builtin_bit_cast(Piece, load_words<16>(place(va, pa[i])));
+#pragma unroll
+            for (int i = 0; i < PB; ++i) rb[i] = __builtin_bit_cast(Piece, load_words<16>(place(wb, pb[i])));
+            advance();
+        }
     };
     // the last step's terms past the end are 0, and W's columns past the end stay unread
     auto fetch_checked = [&](int step) {
         const int c0 = step * D;
 #pragma unroll
-        for (int i = 0; i < PA; ++i) ra[i] = load_operand(pa[i] + c0, C - c0 - (int)(threadIdx.x & 7) * E).v;
+        for (int i = 0; i < PA; ++i) ra[i] = load_operand(place(va, pa[i]), C - c0 - (int)(threadIdx.x & 7) * E).v;
 #pragma unroll
         for (int i = 0; i < PB; ++i) {
             if constexpr (TRANS) {
-                const int have = a.cols % E == 0 ? E : a.cols - (n0 + (i * 256 + (int)threadIdx.x) % RPB * E);
-                rb[i] = load_operand(pb[i] + step * step_rows, c0 + kb[i] < C ? have : 0).v;
+                const int piece = i * NT + threadIdx.x;
+                const int have = a.cols % E == 0 ? E : a.cols - (n0 + piece % RPB * E);
+                rb[i] = load_operand(place(wb, pb[i]), c0 + piece / RPB < C ? have : 0).v;
             } else {
-                rb[i] = load_operand(pb[i] + c0, C - c0 - (int)(threadIdx.x & 7) * E).v;
+                rb[i] = load_operand(place(wb, pb[i]), C - c0 - (int)(threadIdx.x & 7) * E).v;
             }
         }
+        advance();
     };
     auto put = [&](int at) {
         char *la = lds + at * (A_BYTES + B_BYTES), *lb = la + A_BYTES;
         const int turned = (threadIdx.x >> 3) * 128 + (((threadIdx.x & 7) ^ (threadIdx.x >> 3 & 7)) << 4);
 #pragma unroll
         for (int i = 0; i < PA; ++i)
-            *reinterpret_cast<Piece *>(la + i * 4096 + turned) = ra[i];
+            *reinterpret_cast<Piece *>(la + i * RT * 128 + turned) = ra[i];
 #pragma unroll
         for (int i = 0; i < PB; ++i) {
-            const int piece = i * 256 + threadIdx.x;
-            char *to = TRANS ? lb + (piece / RPB * BP + piece % RPB * E) * (int)sizeof(T) : lb + i * 4096 + turned;
+            const int piece = i * NT + threadIdx.x;
+            char *to = TRANS ? lb + (piece / RPB * BP + piece % RPB * E) * (int)sizeof(T) : lb + i * RT * 128 + turned;
             *reinterpret_cast<Piece *>(to) = rb[i];
         }
     };
@@ -150,6 +180,76 @@ __global__ __launch_bounds__(256, BM == 256 ? 1 : 2) void project_tiles(WideArgs
     for (int i = 0; i < WM; ++i)
 #pragma unroll
         for (int j = 0; j < WN; ++j) acc[i][j] = f4{0.f, 0.f, 0.f, 0.f};
+
+    // The adapters' part first, while the accumulators are all that is held.
+    int id[WM];
+#pragma unroll
+    for (int i = 0; i < WM; ++i) {
+        const int64_t row = m0 + wm + i * 16 + q;
+        id[i] = a.n && row < a.rows ? a.ids[row] : -1;
+    }
+    bool bad = false;  // one of the lane's rows names an adapter that is not there
+#pragma unroll
+    for (int i = 0; i < WM; ++i) bad |= a.n && id[i] >= a.n;
+    if (a.n && per_split >= a.C) {
+        for (int last = -1;;) {
+            int low = 0x7fffffff;
+#pragma unroll
+            for (int i = 0; i < WM; ++i) low = id[i] > last ? min(low, id[i]) : low;
+            const int cur = next_adapter(low, last);
+            if (cur >= a.n) break;
+            last = cur;
+            const float sc = !TRANS && a.scale ? a.scale[cur] : 1.f;
+            const T *f = reinterpret_cast<const T *>(a.f) + (int64_t)cur * a.cols * a.r;
+            constexpr int Q = sizeof(T) == 2 ? 3 : 1, H = WM < 4 ? WM : 4;
+            for (int k0 = 0; k0 < a.r; k0 += kStep<T>) {
+                const int k = k0 + g * E;
+                // Whole operands lie inside or outside the rank: loads without
+                // branches, all in flight together.
+                const bool even = a.r % E == 0;
+                const int at = even ? min(k, a.r - E) : k, have = even ? E : a.r - k;
+                Operand<T> of[WN];
+#pragma unroll
+                for (int j = 0; j < WN; ++j) {
+                    const int col = min(n0 + wn + j * 16 + q, a.cols - 1);
+                    of[j] = TRANS ? gather_operand(f + (int64_t)at * a.cols + col, a.cols, have)
+                                  : load_operand(f + (int64_t)col * a.r + at, have);
+                }
+#pragma unroll
+                for (int h = 0; h < WM; h += H) {
+                    float tv[H][E];
+#pragma unroll
+                    for (int i = 0; i < H; ++i) {
+                        const float *t = a.t + clamp_row(m0 + wm + (h + i) * 16 + q, a.rows) * a.r + at;
+                        if (even) {
+#pragma unroll
+                            for (int e = 0; e < E; e += 4) unpack<float, 4>(load_words<16>(t + e), tv[i] + e);
+                        } else {
+#pragma unroll
+                            for (int e = 0; e < E; ++e) tv[i][e] = e < have ? t[e] : 0.f;
+                        }
+                    }
+#pragma unroll
+                    for (int i = 0; i < H; ++i) {
+                        const bool hit = id[h + i] == cur;
+                        if (!__any(hit)) continue;
+                        Operand<T> ot[Q];
+#pragma unroll
+                        for (int e = 0; e < E; ++e) tv[i][e] = k < a.r ? tv[i][e] * sc : 0.f;
+                        split_operand(tv[i], ot);
+#pragma unroll
+                        for (int j = 0; j < WN; ++j) {
+                            f4 z = f4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                            for (int p = 0; p < Q; ++p) z = block_product(of[j], ot[p], z);
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) acc[h + i][j][e] += hit ? z[e] : 0.f;
+                        }
+                    }
+                }
+            }
+        }
+    }
 
     auto read = [&](int at, int half, Operand<T>(&oa)[WM], Operand<T>(&ob)[WN]) {
         const char *la = lds + at * (A_BYTES + B_BYTES), *lb = la + A_BYTES;
@@ -190,33 +290,46 @@ __global__ __launch_bounds__(256, BM == 256 ? 1 : 2) void project_tiles(WideArgs
     // steps that are read without checks
     const int whole = TRANS && a.cols % E != 0 && n0 + BN > a.cols ? 0 : C / D;
     auto get = [&](int step) {
-        if (step < whole) fetch(step);
+        if (BUFFER || step < whole) fetch();
         else if (step < steps) fetch_checked(step);
     };
     get(0);
     put(0);
     get(1);
     __syncthreads();
-    Operand<T> oa[2][WM], ob[2][WN];
-    read(0, 0, oa[0], ob[0]);
     int s = 0;
-    for (; s + 2 < whole; ++s) {
-        put((s + 1) & 1);
-        fetch(s + 2);
-        read(s & 1, 1, oa[1], ob[1]);
-        products(oa[0], ob[0]);
-        __syncthreads();
-        read((s + 1) & 1, 0, oa[0], ob[0]);
-        products(oa[1], ob[1]);
-    }
-    for (; s < steps; ++s) {
-        if (s + 1 < steps) put((s + 1) & 1);
-        get(s + 2);
-        read(s & 1, 1, oa[1], ob[1]);
-        products(oa[0], ob[0]);
-        __syncthreads();
-        if (s + 1 < steps) read((s + 1) & 1, 0, oa[0], ob[0]);
-        products(oa[1], ob[1]);
+    if constexpr (AHEAD) {
+        Operand<T> oa[2][WM], ob[2][WN];
+        read(0, 0, oa[0], ob[0]);
+        for (; s + 2 < whole; ++s) {
+            put((s + 1) & 1);
+            fetch();
+            read(s & 1, 1, oa[1], ob[1]);
+            products(oa[0], ob[0]);
+            __syncthreads();
+            read((s + 1) & 1, 0, oa[0], ob[0]);
+            products(oa[1], ob[1]);
+        }
+        for (; s < steps; ++s) {
+            if (s + 1 < steps) put((s + 1) & 1);
+            get(s + 2);
+            read(s & 1, 1, oa[1], ob[1]);
+            products(oa[0], ob[0]);
+            __syncthreads();
+            if (s + 1 < steps) read((s + 1) & 1, 0, oa[0], ob[0]);
+            products(oa[1], ob[1]);
+        }
+    } else {
+        Operand<T> oa[WM], ob[WN];
+        for (; s < steps; ++s) {
+            put((s + 1) & 1);
+            fetch();
+            read(s & 1, 0, oa, ob);
+            products(oa, ob);
+            read(s & 1, 1, oa, ob);
+            products(oa, ob);
+            __syncthreads();
+        }
     }
 
     if (per_split < a.C) {
@@ -240,56 +353,6 @@ __global__ __launch_bounds__(256, BM == 256 ? 1 : 2) void project_tiles(WideArgs
         return;
     }
 
-    // the adapters' part
-    int id[WM];
-#pragma unroll
-    for (int i = 0; i < WM; ++i) {
-        const int64_t row = m0 + wm + i * 16 + q;
-        id[i] = a.n && row < a.rows ? a.ids[row] : -1;
-    }
-    if (a.n) {
-        for (int last = -1;;) {
-            int low = 0x7fffffff;
-#pragma unroll
-            for (int i = 0; i < WM; ++i) low = id[i] > last ? min(low, id[i]) : low;
-            const int cur = next_adapter(low, last);
-            if (cur >= a.n) break;
-            last = cur;
-            const float sc = !TRANS && a.scale ? a.scale[cur] : 1.f;
-            const T *f = reinterpret_cast<const T *>(a.f) + (int64_t)cur * a.cols * a.r;
-            constexpr int Q = sizeof(T) == 2 ? 3 : 1;
-#pragma unroll
-            for (int i = 0; i < WM; ++i) {
-                if (!__any(id[i] == cur)) continue;
-                f4 z[WN];
-#pragma unroll
-                for (int j = 0; j < WN; ++j) z[j] = f4{0.f, 0.f, 0.f, 0.f};
-                const float *t = a.t + clamp_row(m0 + wm + i * 16 + q, a.rows) * a.r;
-                for (int k0 = 0; k0 < a.r; k0 += kStep<T>) {
-                    const int k = k0 + g * E;
-                    float tv[E];
-#pragma unroll
-                    for (int e = 0; e < E; ++e) tv[e] = k + e < a.r ? t[k + e] * sc : 0.f;
-                    Operand<T> ot[Q];
-                    split_operand(tv, ot);
-#pragma unroll
-                    for (int j = 0; j < WN; ++j) {
-                        const int col = min(n0 + wn + j * 16 + q, a.cols - 1);
-                        const Operand<T> of = TRANS ? gather_operand(f + (int64_t)k * a.cols + col, a.cols, a.r - k)
-                                                    : load_operand(f + (int64_t)col * a.r + k, a.r - k);
-#pragma unroll
-                        for (int p = 0; p < Q; ++p) z[j] = block_product(of, ot[p], z[j]);
-                    }
-                }
-                const bool hit = id[i] == cur;
-#pragma unroll
-                for (int j = 0; j < WN; ++j)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) acc[i][j][e] += hit ? z[j][e] : 0.f;
-            }
-        }
-    }
-
 #pragma unroll
     for (int j = 0; j < WN; ++j) {
         const int col = n0 + wn + j * 16 + g * 4;
@@ -300,9 +363,10 @@ __global__ __launch_bounds__(256, BM == 256 ? 1 : 2) void project_tiles(WideArgs
         for (int i = 0; i < WM; ++i) {
             const int64_t row = m0 + wm + i * 16 + q;
             if (row >= a.rows) continue;
+            const bool wrong = bad && a.ids[row] >= a.n;
             float out[4];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) out[e] = a.n && id[i] >= a.n ? NAN : acc[i][j][e] + bias[e];
+            for (int e = 0; e < 4; ++e) out[e] = wrong ? NAN : acc[i][j][e] + bias[e];
             T *to = reinterpret_cast<T *>(a.out) + row * a.os + col;
             if (col + 4 <= a.cols) store_words<4 * sizeof(T)>(to, pack<T, 4>(out));
             else {
@@ -371,7 +435,7 @@ __global__ __launch_bounds__(256) void project_join(WideArgs a, int splits)
     }
 }
 
-template <typename T, bool TRANS, int BM, int BN>
+template <typename T, bool TRANS, int BM, int BN, int WR, int WC>
 hipError_t go(const WideArgs &a, int splits, int per_split, hipStream_t s)
 {
     const int64_t tm = (a.rows + BM - 1) / BM;
@@ -389,7 +453,7 @@ hipError_t go(const WideArgs &a, int splits, int per_split, hipStream_t s)
             p.t = a.t + row * a.r;
             p.ids = a.ids + row;
         }
-        hipLaunchKernelGGL((project_tiles<T, TRANS, BM, BN>), dim3((unsigned)(m * tn), splits), dim3(256), 0, s,
+        hipLaunchKernelGGL((project_tiles<T, TRANS, BM, BN, WR, WC>), dim3((unsigned)(m * tn), splits), dim3(64 * WR * WC), 0, s,
                            p, (int)m, tn, per_split);
         hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
@@ -404,11 +468,12 @@ struct WidePlan {
 // 128 x 128 tiles where they give every CU one, else 64 x 64 ones; where even
 // these leave CUs idle the summed axis is split in stretches of four steps or
 // more (a launch more, and the parts' way through memory).
-WidePlan wide_plan(int64_t rows, int cols, int C, int dtype)
+WidePlan wide_plan(int64_t rows, int cols, int C, int dtype, bool large)
 {
     const auto tiles = [&](int b) { return ((rows + b - 1) / b) * ((cols + b - 1) / b); };
     WidePlan p{64, 1, C};
-    if (tiles(128) >= 256) p.tile = 128;
+    if (large && dtype == DT_BF16 && tiles(256) >= 192) p.tile = 256;
+    else if (tiles(128) >= 256) p.tile = 128;
     else if (tiles(64) < 256) {
         const int depth = dtype == DT_BF16 ? 64 : 32, steps = (C + depth - 1) / depth;
         const int splits = (int)std::min<int64_t>((512 + tiles(64) - 1) / tiles(64), steps / 4);
@@ -423,9 +488,15 @@ WidePlan wide_plan(int64_t rows, int cols, int C, int dtype)
 template <typename T, bool TRANS>
 hipError_t run(const WideArgs &a, int dtype, hipStream_t s)
 {
-    const WidePlan p = wide_plan(a.rows, a.cols, a.C, dtype);
-    if (p.tile == 128) return go<T, TRANS, 128, 128>(a, 1, a.C, s);
-    hipError_t e = go<T, TRANS, 64, 64>(a, p.splits, p.per_split, s);
+    const auto apart = [](const void *p, int64_t stride, int64_t rows) {
+        return ((uintptr_t)p & 15) == 0 && stride * sizeof(T) % 16 == 0 && stride * (int64_t)sizeof(T) * rows < (1ll << 31);
+    };
+    const bool large = apart(a.v, a.vs, 256) && a.C % 64 == 0 && (!TRANS || a.cols % 8 == 0) && apart(a.w, a.ws, TRANS ? a.C + 64 : 256);
+    const WidePlan p = wide_plan(a.rows, a.cols, a.C, dtype, large);
+    if constexpr (sizeof(T) == 2)
+        if (p.tile == 256) return go<T, TRANS, 256, 256, 2, 4>(a, 1, a.C, s);
+    if (p.tile == 128) return go<T, TRANS, 128, 128, 2, 2>(a, 1, a.C, s);
+    hipError_t e = go<T, TRANS, 64, 64, 2, 2>(a, p.splits, p.per_split, s);
     if (e != hipSuccess || p.splits == 1) return e;
     hipLaunchKernelGGL((project_join<T, TRANS>), dim3(grid_of((a.rows * ((a.cols + 3) / 4) + 255) / 256)), dim3(256), 0, s, a,
                        p.splits);
@@ -436,7 +507,7 @@ hipError_t run(const WideArgs &a, int dtype, hipStream_t s)
 
 size_t wide_parts(int64_t rows, int cols, int C, int dtype)
 {
-    const WidePlan p = wide_plan(rows, cols, C, dtype);
+    const WidePlan p = wide_plan(rows, cols, C, dtype, false);
     return p.splits > 1 ? (size_t)p.splits * rows * cols * sizeof(float) : 0;
 }
 

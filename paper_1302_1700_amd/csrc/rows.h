@@ -58,13 +58,8 @@ hipError_t launch_project_grad(const ProjArgs &a, int dtype, const void *g, int6
 
 __device__ __forceinline__ float to_f32(float v) { return v; }
 __device__ __forceinline__ float to_f32(uint16_t v) { return __uint_as_float((uint32_t)v << 16); }
-// bf16, round to nearest even; a NaN keeps its sign and becomes quiet
-__device__ __forceinline__ uint16_t to_bf16(float f)
-{
-    const uint32_t u = __float_as_uint(f);
-    if ((u & 0x7fffffffu) > 0x7f800000u) return (uint16_t)((u >> 16) | 0x40);
-    return (uint16_t)((u + 0x7fffu + ((u >> 16) & 1)) >> 16);
-}
+// bf16, round to nearest even (the hardware's conversion)
+__device__ __forceinline__ uint16_t to_bf16(float f) { return __builtin_bit_cast(uint16_t, (__bf16)f); }
 __device__ __forceinline__ void store_as(float *p, float v) { *p = v; }
 __device__ __forceinline__ void store_as(uint16_t *p, float v) { *p = to_bf16(v); }
 

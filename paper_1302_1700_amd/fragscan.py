@@ -423,31 +423,39 @@ def _row_out(t, name, like, shape):
 
 
 class _On:
-    """The device and stream of a call: the tensors' device is made the current
-    one if it is not, and what the call allocates belongs to its stream."""
+    """The device and stream of a call made the current ones, so that what the
+    call allocates belongs to its stream."""
 
     def __init__(self, t, stream):
         import torch
-        if not t.is_cuda:
-            raise ValueError("the tensors must be on a GPU")
         if stream is not None and stream.device != t.device:
             raise ValueError("the stream is on %s, the tensors on %s" % (stream.device, t.device))
-        self._in = []
-        if torch.cuda.current_device() != t.device.index:
-            self._in.append(torch.cuda.device(t.device))
-        if stream is not None:
-            self._in.append(torch.cuda.stream(stream))
+        self._in = [torch.cuda.device(t.device)] + ([torch.cuda.stream(stream)] if stream is not None else [])
 
     def __enter__(self):
-        import torch
         for c in self._in:
             c.__enter__()
-        return torch.cuda.current_stream().cuda_stream
 
     def __exit__(self, *exc):
         for c in reversed(self._in):
             c.__exit__(*exc)
         return False
+
+
+def _elsewhere(t, stream):
+    """Whether a call on t needs _On: a stream is given, or t's device is not the current one."""
+    import torch
+    if not t.is_cuda:
+        raise ValueError("the tensors must be on a GPU")
+    return stream is not None or torch.cuda.current_device() != t.device.index
+
+
+def _current_stream(device):
+    """Handle of the device's current stream (torch.cuda.current_stream, which
+    wraps the same handle in an object, takes 2.8 us of a call's 10)."""
+    import torch
+    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    return raw(device.index) if raw else torch.cuda.current_stream(device).cuda_stream
 
 
 def _row_workspace(nbytes, given, device):
@@ -472,24 +480,26 @@ def logprobs(scores, labels=None, n_top=0, temperature=1.0, workspace=None, stre
     import torch
     lib = load()
     dt = _row_dtype(scores, "scores")
-    rows, V, stride = _rows_of(scores, "scores")
+    rows, V, row_stride = _rows_of(scores, "scores")
     shape, dev = scores.shape[:-1], scores.device
     n_top = int(n_top)
     if labels is not None:
         _row_array(labels, "labels", torch.int32, shape, dev)
-    with _On(scores, stream) as s:
-        need = ctypes.c_size_t()
-        _check(lib.fs_logprobs_workspace(rows, V, dt, n_top, ctypes.byref(need)), lib)
-        ws, have = _row_workspace(need.value, workspace, dev)
-        f32 = dict(dtype=torch.float32, device=dev)
-        logp = torch.empty(shape, **f32) if labels is not None else None
-        entropy = torch.empty(shape, **f32)
-        norm = torch.empty((*shape, 2), **f32)
-        top_id = torch.empty((*shape, n_top), dtype=torch.int32, device=dev) if n_top else None
-        top_logp = torch.empty((*shape, n_top), **f32) if n_top else None
-        _check(lib.fs_logprobs(scores.data_ptr(), rows, V, stride, dt, float(temperature), _ptr(labels), n_top,
-                               _ptr(logp), entropy.data_ptr(), norm.data_ptr(), _ptr(top_id), _ptr(top_logp),
-                               _ptr(ws), have, s), lib)
+    if _elsewhere(scores, stream):
+        with _On(scores, stream):
+            return logprobs(scores, labels, n_top, temperature, workspace)
+    need = ctypes.c_size_t()
+    _check(lib.fs_logprobs_workspace(rows, V, dt, n_top, ctypes.byref(need)), lib)
+    ws, have = _row_workspace(need.value, workspace, dev)
+    f32 = torch.float32
+    logp = torch.empty(shape, dtype=f32, device=dev) if labels is not None else None
+    entropy = torch.empty(shape, dtype=f32, device=dev)
+    norm = torch.empty((*shape, 2), dtype=f32, device=dev)
+    top_id = torch.empty((*shape, n_top), dtype=torch.int32, device=dev) if n_top else None
+    top_logp = torch.empty((*shape, n_top), dtype=f32, device=dev) if n_top else None
+    _check(lib.fs_logprobs(scores.data_ptr(), rows, V, row_stride, dt, float(temperature), _ptr(labels), n_top,
+                           _ptr(logp), entropy.data_ptr(), norm.data_ptr(), _ptr(top_id), _ptr(top_logp),
+                           _ptr(ws), have, _current_stream(dev)), lib)
     return LogProbs(logp, entropy, norm, top_id, top_logp)
 
 
@@ -502,48 +512,47 @@ def logprobs_grad(scores, norm, labels=None, g_logp=None, entropy=None, g_entrop
     import torch
     lib = load()
     dt = _row_dtype(scores, "scores")
-    rows, V, stride = _rows_of(scores, "scores")
+    rows, V, row_stride = _rows_of(scores, "scores")
     shape, dev = scores.shape[:-1], scores.device
     given = [_row_array(norm, "norm", torch.float32, (*shape, 2), dev)]
     for t, name, kind in ((labels, "labels", torch.int32), (entropy, "entropy", torch.float32),
                           (g_logp, "g_logp", torch.float32), (g_entropy, "g_entropy", torch.float32)):
         given.append(None if t is None else _row_array(t, name, kind, shape, dev))
     norm_p, labels_p, entropy_p, g_logp_p, g_entropy_p = given
-    with _On(scores, stream) as s:
-        out, g_stride = _row_out(out, "out", scores, tuple(scores.shape))
-        _check(lib.fs_logprobs_grad(scores.data_ptr(), rows, V, stride, dt, float(temperature), labels_p, norm_p,
-                                    entropy_p, g_logp_p, g_entropy_p, out.data_ptr(), g_stride, s), lib)
+    if _elsewhere(scores, stream):
+        with _On(scores, stream):
+            return logprobs_grad(scores, norm, labels, g_logp, entropy, g_entropy, temperature, out)
+    out, g_stride = _row_out(out, "out", scores, scores.shape)
+    _check(lib.fs_logprobs_grad(scores.data_ptr(), rows, V, row_stride, dt, float(temperature), labels_p, norm_p,
+                                entropy_p, g_logp_p, g_entropy_p, out.data_ptr(), g_stride, _current_stream(dev)), lib)
     return out
 
 
 def _projection(x, weight, bias, adapters, ids):
     import torch
     dt = _row_dtype(x, "x")
-    rows, K, stride = _rows_of(x, "x")
+    rows, K, x_stride = _rows_of(x, "x")
     dev = x.device
     if weight.dim() != 2 or weight.shape[1] != K or weight.dtype != x.dtype or weight.device != dev:
         raise ValueError("weight must be a %s tensor [m, %d] on %s" % (str(x.dtype)[6:], K, dev))
     M, _, w_stride = _rows_of(weight, "weight")
-    p = fs_projection(rows=rows, k=K, m=M, dtype=dt, d_x=x.data_ptr(), x_stride=stride, d_w=weight.data_ptr(),
-                      w_stride=w_stride)
-    if bias is not None:
-        p.d_bias = _row_array(bias, "bias", torch.float32, (M,), dev)
+    bias_p = None if bias is None else _row_array(bias, "bias", torch.float32, (M,), dev)
     if adapters is not None:
         a, b, scale = adapters
         if a.dim() != 3 or b.dim() != 3 or a.shape[0] < 1 or a.shape[1] < 1:
             raise ValueError("adapters must be a [n, rank, k] and b [n, m, rank], neither empty")
         n, r = a.shape[:2]
-        p.n_adapters, p.rank = n, r
-        p.d_a = _row_array(a, "adapters' a", x.dtype, (n, r, K), dev)
-        p.d_b = _row_array(b, "adapters' b", x.dtype, (n, M, r), dev)
-        if scale is not None:
-            p.d_scale = _row_array(scale, "adapters' scale", torch.float32, (n,), dev)
         if ids is None:
             raise ValueError("adapters need ids")
-        p.d_ids = _row_array(ids, "ids", torch.int32, x.shape[:-1], dev)
+        low_rank = (_row_array(a, "adapters' a", x.dtype, (n, r, K), dev),
+                    _row_array(b, "adapters' b", x.dtype, (n, M, r), dev),
+                    None if scale is None else _row_array(scale, "adapters' scale", torch.float32, (n,), dev),
+                    _row_array(ids, "ids", torch.int32, x.shape[:-1], dev))
     elif ids is not None:
         raise ValueError("ids without adapters")
-    return p
+    else:
+        n, r, low_rank = 0, 0, (None, None, None, None)
+    return fs_projection(rows, K, M, dt, n, r, x.data_ptr(), x_stride, weight.data_ptr(), w_stride, bias_p, *low_rank)
 
 
 def project(x, weight, bias=None, adapters=None, ids=None, out=None, return_hidden=False, workspace=None, stream=None):
@@ -557,13 +566,17 @@ def project(x, weight, bias=None, adapters=None, ids=None, out=None, return_hidd
     p = _projection(x, weight, bias, adapters, ids)
     if return_hidden and adapters is None:
         raise ValueError("return_hidden without adapters")
-    with _On(x, stream) as s:
-        need = ctypes.c_size_t()
-        _check(lib.fs_project_workspace(ctypes.byref(p), ctypes.byref(need)), lib)
-        ws, have = _row_workspace(need.value, workspace, x.device)
-        out, y_stride = _row_out(out, "out", x, (*x.shape[:-1], p.m))
-        hidden = torch.empty((*x.shape[:-1], p.rank), dtype=torch.float32, device=x.device) if return_hidden else None
-        _check(lib.fs_project(ctypes.byref(p), out.data_ptr(), y_stride, _ptr(hidden), _ptr(ws), have, s), lib)
+    if _elsewhere(x, stream):
+        with _On(x, stream):
+            return project(x, weight, bias, adapters, ids, out, return_hidden, workspace)
+    need, dev = ctypes.c_size_t(), x.device
+    _check(lib.fs_project_workspace(ctypes.byref(p), ctypes.byref(need)), lib)
+    ws, have = _row_workspace(need.value, workspace, dev)
+    shape = x.shape[:-1]
+    out, y_stride = _row_out(out, "out", x, (*shape, p.m))
+    hidden = torch.empty((*shape, p.rank), dtype=torch.float32, device=dev) if return_hidden else None
+    _check(lib.fs_project(ctypes.byref(p), out.data_ptr(), y_stride, _ptr(hidden), _ptr(ws), have,
+                          _current_stream(dev)), lib)
     return (out, hidden) if return_hidden else out
 
 
@@ -586,13 +599,15 @@ def project_grad(g, x, weight, adapters=None, ids=None, hidden=None, need_x=True
         if adapters is None:
             raise ValueError("hidden without adapters")
         h = _row_array(hidden, "hidden", torch.float32, (*x.shape[:-1], p.rank), x.device)
-    with _On(x, stream) as s:
-        need = ctypes.c_size_t()
-        _check(lib.fs_project_grad_workspace(ctypes.byref(p), ctypes.byref(need)), lib)
-        ws, have = _row_workspace(need.value, workspace, x.device)
-        gx = torch.empty(x.shape, dtype=x.dtype, device=x.device) if need_x else None
-        ga = torch.empty_like(adapters.a) if need_adapters else None
-        gb = torch.empty_like(adapters.b) if need_adapters else None
-        _check(lib.fs_project_grad(ctypes.byref(p), g.data_ptr(), g_stride, h, _ptr(gx), p.k, _ptr(ga), _ptr(gb),
-                                   _ptr(ws), have, s), lib)
+    if _elsewhere(x, stream):
+        with _On(x, stream):
+            return project_grad(g, x, weight, adapters, ids, hidden, need_x, need_adapters, workspace)
+    need, dev = ctypes.c_size_t(), x.device
+    _check(lib.fs_project_grad_workspace(ctypes.byref(p), ctypes.byref(need)), lib)
+    ws, have = _row_workspace(need.value, workspace, dev)
+    gx = torch.empty(x.shape, dtype=x.dtype, device=dev) if need_x else None
+    ga = torch.empty_like(adapters.a) if need_adapters else None
+    gb = torch.empty_like(adapters.b) if need_adapters else None
+    _check(lib.fs_project_grad(ctypes.byref(p), g.data_ptr(), g_stride, h, _ptr(gx), p.k, _ptr(ga), _ptr(gb),
+                               _ptr(ws), have, _current_stream(dev)), lib)
     return gx, ga, gb
