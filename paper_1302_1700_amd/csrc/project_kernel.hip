@@ -20,7 +20,7 @@ template <bool GATHER, typename T, int RB, int NB>
 __device__ __forceinline__ void row_products(const T *const (&row)[RB], const T *const (&col)[NB], int64_t col_step,
                                              int c0, int c1, f4 (&acc)[RB][NB])
 {
-    constexpr int E = Operand<T>::kE, U = NB == 1 ? 4 : 2;  // steps whose loads are in flight together
+    constexpr int E = Operand<T>::kE, U = NB == 1 && !GATHER ? 8 / RB : NB <= 2 ? 4 / RB : 2;  // steps whose loads are in flight together
     const int g = (threadIdx.x & 63) >> 4;
     auto load = [&](int c, int have, Operand<T>(&oa)[RB], Operand<T>(&ob)[NB]) {
 #pragma unroll
@@ -460,7 +460,13 @@ __global__ __launch_bounds__(256) void factor_join(FactorArgs<T> a)
         for (int at = 0; at < a.runs; at += 1024) {
             const int total = list_rows<4>(a.used + (int64_t)i * a.runs, at, a.runs, 1, list, count, [](int64_t, int) {});
             const int quarter = (total + 3) / 4, to = std::min(total, (wave + 1) * quarter);
-            for (int l = wave * quarter; l < to; ++l) s += parts[(int64_t)(at + list[l]) * per_adapter];
+            for (int l = wave * quarter; l < to; l += 8) {
+                float v[8];  // in flight together
+#pragma unroll
+                for (int k = 0; k < 8; ++k) v[k] = parts[(int64_t)(at + list[std::min(l + k, to - 1)]) * per_adapter];
+#pragma unroll
+                for (int k = 0; k < 8; ++k) s += l + k < to ? v[k] : 0.f;
+            }
         }
         __syncthreads();
         sums[wave][lane] = s;
@@ -485,7 +491,7 @@ bool narrow(const ProjArgs &a) { return a.M + a.r <= 64; }
 template <typename T>
 int axis_waves(int64_t rows, int C)
 {
-    if (rows <= 256 && C >= 32 * kStep<T>) return 16;
+    if (rows <= 8192 && C >= 32 * kStep<T>) return 16;
     return rows <= 16 * 4096 && C >= 8 * kStep<T> ? 4 : 1;
 }
 
@@ -502,7 +508,7 @@ RunPlan run_plan(const ProjArgs &a)
 {
     const int64_t ctiles = both(a) ? (a.K + 255) / 256 : (a.K + 255) / 256 + (a.M + 255) / 256;
     const double part = (double)a.n * a.r * (a.K + a.M) * sizeof(float);
-    int64_t runs = std::max<int64_t>(1, std::min<int64_t>(2048 / ctiles, a.rows / 256));
+    int64_t runs = std::max<int64_t>(1, std::min<int64_t>(2048 / ctiles, a.rows / 128));
     runs = std::max<int64_t>(1, std::min<int64_t>(runs, (int64_t)(268435456.0 / part)));
     RunPlan p;
     p.run_rows = (int)(((a.rows + runs - 1) / runs + 63) / 64 * 64);
@@ -519,9 +525,10 @@ hipError_t go_rank(const T *v, int64_t vs, int64_t rows, int C, const T *f, int 
                    const int *ids, float *t, hipStream_t s)
 {
     const int waves = axis_waves<T>(rows, C);
-    // 64 sixteens of 1024 rows over the workgroups of an adapter: one each where
-    // there are few adapters, fewer workgroups where the rows spread over many
-    const int per = waves == 1 ? 4 : 1, most = (int)std::min<int64_t>(64, (rows + 15) / 16);
+    // The 64 sixteens of 1024 rows over the workgroups of an adapter: up to two
+    // each where there are few adapters, fewer workgroups where the rows spread
+    // over many (a workgroup without rows costs the look at their ids).
+    const int per = waves == 1 ? 4 : 1, most = (int)std::min<int64_t>(32, (rows + 15) / 16);
     const int slots = std::max(1, std::min(most, std::max(4, 512 / n)) / per);
     const RankArgs<T> a{v, f, vs, rows, C, n, r, slots, scale, ids, t};
     const dim3 grid(slots, (unsigned)std::min<int64_t>((rows + 1023) / 1024 * n, 65535));

@@ -390,18 +390,28 @@ __global__ __launch_bounds__(256) void project_join(WideArgs a, int splits)
         const int64_t row = k / quads;
         const int col = (int)(k - row * quads) * 4, have = min(4, a.cols - col);
         float y[4] = {0.f, 0.f, 0.f, 0.f}, z[4] = {0.f, 0.f, 0.f, 0.f};
-        for (int s = 0; s < splits; ++s) {
-            const float *p = a.parts + (s * a.rows + row) * a.cols + col;
-            if (have == 4) {
-                float v[4];
-                unpack<float, 4>(load_words<16>(p), v);
+        for (int s0 = 0; s0 < splits; s0 += 8) {
+            float v[8][4];  // in flight together
 #pragma unroll
-                for (int e = 0; e < 4; ++e) y[e] += v[e];
-            } else {
+            for (int s = 0; s < 8; ++s) {
+                const float *p = a.parts + ((int64_t)min(s0 + s, splits - 1) * a.rows + row) * a.cols;
+                if (a.cols >= 4) {
+                    // the last columns from further left, moved into place below
+                    unpack<float, 4>(load_words<16>(p + min(col, a.cols - 4)), v[s]);
+                } else {
 #pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    if (e < have) y[e] += p[e];
+                    for (int e = 0; e < 4; ++e) v[s][e] = e < have ? p[col + e] : 0.f;
+                }
             }
+#pragma unroll
+            for (int s = 0; s < 8; ++s)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) y[e] += s0 + s < splits ? v[s][e] : 0.f;
+        }
+        if (have < 4 && a.cols >= 4) {
+            const int move = 4 - have;
+#pragma unroll
+            for (int e = 0; e < 3; ++e) y[e] = e + move < 4 ? (move == 1 ? y[e + 1] : move == 2 ? y[(e + 2) & 3] : y[3]) : 0.f;
         }
         const int id = a.n ? a.ids[row] : -1;
         if (id >= 0 && id < a.n) {
@@ -465,18 +475,19 @@ struct WidePlan {
     int tile, splits, per_split;
 };
 
-// 128 x 128 tiles where they give every CU one, else 64 x 64 ones; where even
-// these leave CUs idle the summed axis is split in stretches of four steps or
-// more (a launch more, and the parts' way through memory).
+// 256 x 256 tiles where three CUs in four get one, 128 x 128 ones where each
+// does, else 64 x 64 ones; where these are fewer than two a CU the summed axis
+// is split in stretches of four steps or more (a launch more, and the parts'
+// way through memory).
 WidePlan wide_plan(int64_t rows, int cols, int C, int dtype, bool large)
 {
     const auto tiles = [&](int b) { return ((rows + b - 1) / b) * ((cols + b - 1) / b); };
     WidePlan p{64, 1, C};
     if (large && dtype == DT_BF16 && tiles(256) >= 192) p.tile = 256;
     else if (tiles(128) >= 256) p.tile = 128;
-    else if (tiles(64) < 256) {
+    else if (tiles(64) < 512) {
         const int depth = dtype == DT_BF16 ? 64 : 32, steps = (C + depth - 1) / depth;
-        const int splits = (int)std::min<int64_t>((512 + tiles(64) - 1) / tiles(64), steps / 4);
+        const int splits = (int)std::min<int64_t>((511 + tiles(64)) / tiles(64), steps / 4);
         if (splits > 1) {
             p.per_split = (steps + splits - 1) / splits * depth;
             p.splits = (C + p.per_split - 1) / p.per_split;
