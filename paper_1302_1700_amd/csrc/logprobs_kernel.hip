@@ -188,47 +188,26 @@ __global__ __launch_bounds__(256) void logprobs_short(LogprobArgs a)
     }
 }
 
-// The n best scores so far, best first, one in each of the wave's lanes.
-// A new score goes in behind its equals (scores come in the order of their
-// classes): the lanes from its place on take over from the lane before.
-struct Best {
-    float v;
-    int id;
-    __device__ __forceinline__ void insert(float nv, int nid, int lane)
-    {
-        const int place = __popcll(__ballot(v >= nv));
-        const float uv = __shfl_up(v, 1);
-        const int uid = __shfl_up(id, 1);
-        v = lane < place ? v : lane == place ? nv : uv;
-        id = lane < place ? id : lane == place ? nid : uid;
-    }
-};
-
 __device__ __forceinline__ float lane_value(float v, int lane)
 {
     return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v), lane));
 }
 
-// The n-th largest of the wave's values (n <= 64).
-__device__ __forceinline__ float nth_largest(float v, int n, int lane)
+// The n-th and the k-th largest of the wave's values (n, k <= 64), equal ones
+// counted each: the smallest value that fewer than n (k) exceed.
+__device__ __forceinline__ void nth_largest(float v, int n, int k, float *nth, float *kth)
 {
-    int before = 0;
+    int above = 0;
 #pragma unroll
-    for (int o = 0; o < 64; ++o) {
-        const float w = lane_value(v, o);
-        before += (w > v || (w == v && o < lane)) ? 1 : 0;
+    for (int o = 0; o < 64; ++o) above += lane_value(v, o) > v ? 1 : 0;
+    float a = above < n ? v : INFINITY, b = above < k ? v : INFINITY;
+#pragma unroll
+    for (int d = 32; d; d >>= 1) {
+        a = fminf(a, __shfl_xor(a, d));
+        b = fminf(b, __shfl_xor(b, d));
     }
-    const uint64_t at = __ballot(before == n - 1);
-    return at ? lane_value(v, __ffsll((unsigned long long)at) - 1) : -INFINITY;  // none: NaNs among them
-}
-
-// The next float below v: "above it" is "at least v".
-__device__ __forceinline__ float just_below(float v)
-{
-    v += 0.0f;
-    const uint32_t u = __float_as_uint(v);
-    if (v == -INFINITY) return v;
-    return __uint_as_float(v > 0.f ? u - 1 : v < 0.f ? u + 1 : 0x80000001u);
+    *nth = a;
+    *kth = b;
 }
 
 // Joins sorted lists of n keys each (in LDS, `lists` of them, 0 past their
@@ -271,153 +250,225 @@ __device__ __forceinline__ void join_lists(const LogprobArgs &a, int64_t row, co
     }
 }
 
+// The best classes of a long row, or of a run of it, that the threads of a
+// workgroup have just gone through (element (i W + wave) U + u, times 64, plus
+// lane, is the i U + u-th run of N scores of a thread).  Every thread knows its
+// largest score.  n scores reach the n-th largest of these in a wave, and n / W
+// of every wave the (n / W)-th largest of its own: the larger of the best of the
+// first and the worst of the second bounds the n best from below, so only the
+// few threads whose largest reaches it hold any of them.  Their scores are read
+// once more, a run a thread, and those that reach the bound are listed as keys
+// and placed by counting larger keys.  Where more than the list holds reach it (equal scores,
+// or many of the best in one thread's hands) the list is cut to its n best and
+// its last key is the new bound, as often as it takes.
+constexpr int kList = 1024;  // a wave's runs hold up to 512
+
+template <int W>
+struct TopLds {
+    uint64_t list[kList + 64], sorted[64];
+    int flagged[64 * W], counts[W];
+    float one[W], all[W];  // the waves' bounds
+};
+
+template <typename T, int W, int U>
+__device__ __forceinline__ int find_top(TopLds<W> &l, const T *x, int first, int V, float largest, int n)
+{
+    constexpr int N = kVec<T>, NT = 64 * W;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    __syncthreads();  // the unit before has been read
+    float nth, share;
+    nth_largest(largest, n, (n + W - 1) / W, &nth, &share);
+    if (lane == 0) {
+        l.one[wave] = nth;
+        l.all[wave] = share;
+    }
+    __syncthreads();
+    nth = l.one[0];
+    share = l.all[0];
+#pragma unroll
+    for (int w = 1; w < W; ++w) {
+        nth = fmaxf(nth, l.one[w]);
+        share = fminf(share, l.all[w]);
+    }
+    const float t = fmaxf(nth, share);
+    const uint64_t mine = __ballot(largest >= t && largest > -INFINITY);
+    if (lane == 0) l.counts[wave] = __popcll(mine);
+    __syncthreads();
+    int holders = 0, before = 0;
+    for (int w = 0; w < W; ++w) {
+        before += w < wave ? l.counts[w] : 0;
+        holders += l.counts[w];
+    }
+    if (mine >> lane & 1) l.flagged[before + __popcll(mine & ((1ull << lane) - 1))] = threadIdx.x;
+    // keys above `cut` are wanted: scores of at least t, none of -inf
+    uint64_t cut = t == -INFINITY ? score_key(-INFINITY, 0) : score_key(t, 0xffffffffu) - 1;
+    const int batches = (V - first + U * 64 * N - 1) / (U * 64 * N), runs = (batches + W - 1) / W * U;
+    int length = 0;
+    // places of the list's keys among all; keeps the n best
+    auto shorten = [&]() {
+        __syncthreads();
+        for (int q = threadIdx.x; q < length; q += NT) {
+            const uint64_t key = l.list[q];
+            int place = 0;
+#pragma unroll 8
+            for (int o = 0; o < length; ++o) place += l.list[o] > key ? 1 : 0;
+            if (place < n) l.sorted[place] = key;
+        }
+        __syncthreads();
+        length = min(length, n);
+        if ((int)threadIdx.x < length) l.list[threadIdx.x] = l.sorted[threadIdx.x];
+        __syncthreads();
+        if (length == n) cut = max(cut, l.list[n - 1]);
+    };
+    __syncthreads();
+    for (int at = 0; at < holders * runs; at += NT) {
+        const int item = at + (int)threadIdx.x;
+        int j = V;
+        if (item < holders * runs) {
+            const int run = item / holders, who = l.flagged[item - run * holders];
+            const int64_t piece = (int64_t)(run / U * W + (who >> 6)) * U + run % U;
+            j = (int)min((int64_t)V, first + (piece * 64 + (who & 63)) * N);
+        }
+        float v[N];
+        if (j + N <= V) load_run<T, N>(x + j, v);
+        else {
+#pragma unroll
+            for (int e = 0; e < N; ++e) v[e] = j + e < V ? to_f32(x[j + e]) : -INFINITY;
+        }
+        bool pending = true;  // this wave's runs still have to be listed
+        for (;;) {
+            int found = 0;
+#pragma unroll
+            for (int e = 0; e < N; ++e) found += __popcll(__ballot(pending && score_key(v[e], (uint32_t)(j + e)) > cut));
+            if (lane == 0) l.counts[wave] = found;
+            __syncthreads();
+            int start = length, to = length, left = 0;
+            for (int w = 0; w < W; ++w) {
+                const int c = l.counts[w];
+                if (to + c <= kList) {  // as many waves as fit, in order
+                    start += w < wave ? c : 0;
+                    to += c;
+                } else {
+                    left = 1;
+                    if (w <= wave) start = -1;
+                    break;
+                }
+            }
+            __syncthreads();
+            if (start >= 0 && pending) {
+#pragma unroll
+                for (int e = 0; e < N; ++e) {
+                    const uint64_t key = score_key(v[e], (uint32_t)(j + e));
+                    const uint64_t hit = __ballot(key > cut);
+                    if (hit >> lane & 1) l.list[start + __popcll(hit & ((1ull << lane) - 1))] = key;
+                    start += __popcll(hit);
+                }
+                pending = false;
+            }
+            length = to;
+            if (!left) break;
+            shorten();
+        }
+    }
+    shorten();
+    return length;
+}
+
 // What a split of a row leaves for the join: its part, then its keys.
 __host__ __device__ __forceinline__ size_t split_bytes(int n_top) { return 16 + 8 * (size_t)n_top; }
 
 // Long rows: W waves to a row, or to one of `splits` runs of it, each going
-// through batches of kU * 64 * N scores, W batches apart, the next batch's
+// through batches of U * 64 * N scores, W batches apart, the next batch's
 // loads in flight.  A lane keeps its own maximum and sums, moved to the larger
-// maximum once a batch.  The best classes: a batch whose largest score in
-// every lane is at most the wave's n-th best adds nothing (one comparison and
-// a ballot); the first batch starts from the n-th largest of its lanes'
-// maxima, which at least n of its scores reach.
-constexpr int kU = 4;
-
-template <typename T, int W, bool TOP>
+// maximum once a batch.
+template <typename T, int W, int U, bool TOP>
 __global__ __launch_bounds__(64 * W) void logprobs_long(LogprobArgs a, int splits, int per_split, char *parts)
 {
-    constexpr int N = kVec<T>, BATCH = kU * 64 * N;
-    extern __shared__ uint64_t lds_keys[];  // [W][n_top], when W > 1 and TOP
+    constexpr int N = kVec<T>, BATCH = U * 64 * N;
     __shared__ Part lds_part[W];
+    __shared__ TopLds<TOP ? W : 1> top;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const float k = a.inv_t * kLog2e;
     const int n = TOP ? a.n_top : 0;
     const int64_t units = a.rows * splits;
     for (int64_t unit = blockIdx.x; unit < units; unit += gridDim.x) {
-        const int64_t row = splits == 1 ? unit : unit / splits;
-        const int first = (int)(unit - row * splits) * per_split;
+        int64_t row = unit;
+        int first = 0;
+        if (splits > 1) {
+            row = unit / splits;
+            first = (int)(unit - row * splits) * per_split;
+        }
         const int V = min(a.V, first + per_split);  // this run's end
         const T *x = reinterpret_cast<const T *>(a.x) + row * a.stride;
         const int y = a.logp ? a.labels[row] : -1;
         const float xy = y >= 0 && y < a.V ? to_f32(x[y]) : 0.f;
 
         Part p{kLowest, 0.f, 0.f};
-        Best best{-INFINITY, -1};
-        float limit = -INFINITY;
-        bool started = false;
-        typename Words<16>::type next[kU];
+        float largest = -INFINITY;
+        typename Words<16>::type next[U];
         auto fetch = [&](int at) {
+            if (at + BATCH <= V) {
 #pragma unroll
-            for (int u = 0; u < kU; ++u) {
+                for (int u = 0; u < U; ++u) next[u] = load_words<16>(x + at + (u * 64 + lane) * N);
+                return;
+            }
+            for (int u = 0; u < U; ++u) {
                 const int j = at + (u * 64 + lane) * N;
-                if (j + N <= V) next[u] = load_words<16>(x + j);
+                typename Words<16>::type w;
+                if (j + N <= V) w = load_words<16>(x + j);
                 else {
                     float part[N];
 #pragma unroll
                     for (int e = 0; e < N; ++e) part[e] = j + e < V ? to_f32(x[j + e]) : -INFINITY;
-                    next[u] = pack<T, N>(part);
+                    w = pack<T, N>(part);
                 }
+#pragma unroll
+                for (int o = 0; o < U; ++o) next[o] = o == u ? w : next[o];
             }
         };
         int at = first + wave * BATCH;
         if (at < V) fetch(at);
         for (; at < V; at += W * BATCH) {
-            float v[kU * N];
+            float v[U * N];
 #pragma unroll
-            for (int u = 0; u < kU; ++u) unpack<T, N>(next[u], v + u * N);
+            for (int u = 0; u < U; ++u) unpack<T, N>(next[u], v + u * N);
             if (at + W * BATCH < V) fetch(at + W * BATCH);
-            float most[kU], high = -INFINITY;
 #pragma unroll
-            for (int u = 0; u < kU; ++u) {
-                most[u] = v[u * N];
+            for (int e = 0; e < U * N; ++e) largest = fmaxf(largest, v[e]);
+            move_to(p, fmaxf(p.m, largest), k);
 #pragma unroll
-                for (int e = 1; e < N; ++e) most[u] = fmaxf(most[u], v[u * N + e]);
-                high = fmaxf(high, most[u]);
-            }
-            move_to(p, fmaxf(p.m, high), k);
-#pragma unroll
-            for (int e = 0; e < kU * N; ++e) {
+            for (int e = 0; e < U * N; ++e) {
                 const float t = (v[e] - p.m) * k, w = __builtin_amdgcn_exp2f(t);
                 p.s += w;
                 p.d = fmaf(w, fmaxf(t, kFar), p.d);
             }
-            if constexpr (TOP) {
-                if (!started) {
-                    started = true;
-                    limit = just_below(nth_largest(high, n, lane));
-                }
-                if (__ballot(high > limit)) {
-#pragma unroll
-                    for (int u = 0; u < kU; ++u) {
-                        uint64_t who = __ballot(most[u] > limit);
-                        while (who) {
-                            const int l = __ffsll((unsigned long long)who) - 1;
-#pragma unroll
-                            for (int e = 0; e < N; ++e) {
-                                const float nv = lane_value(v[u * N + e], l);
-                                if (nv > limit) {
-                                    best.insert(nv, at + (u * 64 + l) * N + e, lane);
-                                    limit = fmaxf(limit, lane_value(best.v, n - 1));
-                                }
-                            }
-                            who &= who - 1;
-                            who &= __ballot(most[u] > limit);
-                        }
-                    }
-                }
-            }
         }
         p = group_join<64>(p, k);
-        const uint64_t key = TOP && lane < n && best.v != -INFINITY ? score_key(best.v, (uint32_t)best.id) : 0;
         if constexpr (W > 1) {
             __syncthreads();  // the unit before has been read
             if (lane == 0) lds_part[wave] = p;
-            if (TOP && lane < n) lds_keys[wave * n + lane] = key;
             __syncthreads();
             Part q{kLowest, 0.f, 0.f};
             if (lane < W) q = lds_part[lane];
             p = group_join<64>(q, k);
         }
+        RowStats r = finish(p);
+        int listed = 0;
+        if constexpr (TOP)
+            if (!r.bad && !r.empty) listed = find_top<T, W, U>(top, x, first, V, largest, n);
         if (splits > 1) {
             char *to = parts + unit * split_bytes(a.n_top);
             if (threadIdx.x == 0) *reinterpret_cast<Part *>(to) = p;
-            if constexpr (TOP) {
-                uint64_t *out = reinterpret_cast<uint64_t *>(to + 16);
-                if constexpr (W == 1) {
-                    if (lane < n) out[lane] = key;
-                } else {
-                    // the waves' lists joined into one, as join_lists places them
-                    for (int q = threadIdx.x; q < n; q += 64 * W) out[q] = 0;
-                    __syncthreads();
-                    for (int q = threadIdx.x; q < W * n; q += 64 * W) {
-                        const int mine = q / n;
-                        const uint64_t ky = lds_keys[q];
-                        int place = q - mine * n;
-                        for (int l = 0; l < W && place < n && ky; ++l) {
-                            if (l == mine) continue;
-                            int lo = 0, hi = n;
-                            while (lo < hi) {
-                                const int mid = (lo + hi) / 2;
-                                if (lds_keys[l * n + mid] > ky) lo = mid + 1;
-                                else hi = mid;
-                            }
-                            place += lo;
-                        }
-                        if (ky && place < n) out[place] = ky;
-                    }
-                }
-            }
+            if constexpr (TOP)
+                if ((int)threadIdx.x < n)
+                    reinterpret_cast<uint64_t *>(to + 16)[threadIdx.x] =
+                        (int)threadIdx.x < listed ? top.list[threadIdx.x] : 0;
             continue;
         }
-        const RowStats r = finish(p);
         if (threadIdx.x == 0) store_stats(a, row, r, y, xy);
-        if constexpr (TOP) {
-            if constexpr (W == 1) {
-                if (lane < n) store_top(a, row, lane, r, key);
-            } else {
-                join_lists(a, row, r, lds_keys, W);
-            }
-        }
+        if constexpr (TOP)
+            if ((int)threadIdx.x < n)
+                store_top(a, row, threadIdx.x, r, (int)threadIdx.x < listed ? top.list[threadIdx.x] : 0);
     }
 }
 
@@ -515,6 +566,8 @@ __global__ __launch_bounds__(256) void logprobs_grad_short(LogprobGradArgs a)
 }
 
 // Long rows: a workgroup to a piece of kU chunks a thread.
+constexpr int kU = 4;
+
 template <typename T>
 __global__ __launch_bounds__(256) void logprobs_grad_long(LogprobGradArgs a, int pieces)
 {
@@ -540,15 +593,17 @@ struct LongPlan {
     int waves, splits, per_split;
 };
 
+constexpr int kBatch = 4;  // chunks of a batch; 2 where sixteen waves share a row
+
 LongPlan long_plan(int64_t rows, int V, int dtype)
 {
-    const int batch = kU * 64 * (dtype == DT_BF16 ? 8 : 4);
+    const int batch = kBatch * 64 * (dtype == DT_BF16 ? 8 : 4);
     LongPlan p{V <= 2 * batch ? 1 : 4, 1, V};
-    if (rows <= 512 && V > 8 * batch) {
+    if (rows <= 512 && V > 2 * batch) {
         p.waves = 16;
         // runs of two batches a wave, while there are CUs left to take them
         const int most = (int)std::min<int64_t>(64, std::max<int64_t>(1, 512 / rows));
-        p.splits = std::min(most, (V + 32 * batch - 1) / (32 * batch));
+        p.splits = std::min(most, (V + 16 * batch - 1) / (16 * batch));
         if (p.splits > 1) {
             p.per_split = ((V + p.splits - 1) / p.splits + 7) / 8 * 8;
             p.splits = (V + p.per_split - 1) / p.per_split;
@@ -564,13 +619,12 @@ hipError_t go_short(const LogprobArgs &a, hipStream_t s)
     return hipGetLastError();
 }
 
-template <typename T, int W>
+template <typename T, int W, int U>
 hipError_t go_long(const LogprobArgs &a, const LongPlan &p, char *parts, hipStream_t s)
 {
     const dim3 grid(capped(a.rows * p.splits)), block(64 * W);
-    const size_t lds = W > 1 ? (size_t)W * a.n_top * 8 : 0;
-    if (a.n_top) hipLaunchKernelGGL((logprobs_long<T, W, true>), grid, block, lds, s, a, p.splits, p.per_split, parts);
-    else hipLaunchKernelGGL((logprobs_long<T, W, false>), grid, block, 0, s, a, p.splits, p.per_split, parts);
+    if (a.n_top) hipLaunchKernelGGL((logprobs_long<T, W, U, true>), grid, block, 0, s, a, p.splits, p.per_split, parts);
+    else hipLaunchKernelGGL((logprobs_long<T, W, U, false>), grid, block, 0, s, a, p.splits, p.per_split, parts);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || p.splits == 1) return e;
     hipLaunchKernelGGL(logprobs_join<T>, dim3(capped(a.rows)), dim3(256), (size_t)p.splits * a.n_top * 8, s, a, p.splits,
@@ -593,9 +647,9 @@ hipError_t run(const LogprobArgs &a, int dtype, char *parts, hipStream_t s)
     if (V <= 256) return go_short<T, 32, C, N>(a, s);
     if (V <= kShort) return go_short<T, 64, C, N>(a, s);
     const LongPlan p = long_plan(a.rows, V, dtype);
-    if (p.waves == 1) return go_long<T, 1>(a, p, parts, s);
-    if (p.waves == 4) return go_long<T, 4>(a, p, parts, s);
-    return go_long<T, 16>(a, p, parts, s);
+    if (p.waves == 1) return go_long<T, 1, kBatch>(a, p, parts, s);
+    if (p.waves == 4) return go_long<T, 4, kBatch>(a, p, parts, s);
+    return go_long<T, 16, 2>(a, p, parts, s);
 }
 
 template <typename T, int G, int N>
