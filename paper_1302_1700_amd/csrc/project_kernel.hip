@@ -105,7 +105,7 @@ struct RankArgs {
 template <typename T, int NB, int W, bool TRANS>
 __global__ __launch_bounds__(W == 16 ? 1024 : 256) void rank_rows(RankArgs<T> a)
 {
-    constexpr int NW = W == 16 ? 16 : 4, PER = NW / W;
+    constexpr int NW = W == 16 ? 16 : 4, PER = NW / W, RB = W == 1 ? 2 : 1;  // RB sixteens of rows to a product
     __shared__ float part[W > 1 ? W * 256 : 1];
     __shared__ int list[1024], count[16];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, q = lane & 15, g = lane >> 4;
@@ -123,17 +123,20 @@ __global__ __launch_bounds__(W == 16 ? 1024 : 256) void rank_rows(RankArgs<T> a)
         constexpr int S = kStep<T>;
         const int run = W == 1 ? a.C : (a.C + W * S - 1) / (W * S) * S;
         const int c0 = std::min(a.C, wave % W * run), c1 = std::min(a.C, c0 + run);
-        for (int tile = blockIdx.x * PER + wave / W; tile * 16 < total; tile += a.slots * PER) {
-            const T *row[1] = {a.v + (at + list[std::min(tile * 16 + q, total - 1)]) * a.vs};
+        for (int tile = blockIdx.x * PER + wave / W; tile * 16 * RB < total; tile += a.slots * PER) {
+            const T *row[RB];
             const T *col[NB];
-            f4 acc[1][NB];
+            f4 acc[RB][NB];
+#pragma unroll
+            for (int b = 0; b < RB; ++b) row[b] = a.v + (at + list[std::min((tile * RB + b) * 16 + q, total - 1)]) * a.vs;
 #pragma unroll
             for (int j = 0; j < NB; ++j) {
                 const int c = j * 16 + q;
                 col[j] = c >= r ? nullptr : TRANS ? a.f + (int64_t)i * r * a.C + c : a.f + ((int64_t)i * r + c) * a.C;
-                acc[0][j] = f4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int b = 0; b < RB; ++b) acc[b][j] = f4{0.f, 0.f, 0.f, 0.f};
             }
-            row_products<TRANS, T, 1, NB>(row, col, r, c0, c1, acc);
+            row_products<TRANS, T, RB, NB>(row, col, r, c0, c1, acc);
 #pragma unroll
             for (int j = 0; j < NB; ++j) {
                 if constexpr (W > 1) {
@@ -153,19 +156,22 @@ __global__ __launch_bounds__(W == 16 ? 1024 : 256) void rank_rows(RankArgs<T> a)
                 }
                 if (wave % W == 0) {
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const int k = tile * 16 + g * 4 + e;
-                        if (k < total && j * 16 + q < r) a.t[(at + list[k]) * r + j * 16 + q] = acc[0][j][e] * sc;
-                    }
+                    for (int b = 0; b < RB; ++b)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const int k = (tile * RB + b) * 16 + g * 4 + e;
+                            if (k < total && j * 16 + q < r) a.t[(at + list[k]) * r + j * 16 + q] = acc[b][j][e] * sc;
+                        }
                 }
             }
         }
     }
 }
 
-// Few outputs: columns 0 .. M - 1 of the product are W's rows, the next r
-// A_i's; the products go through LDS, where each row's outputs take up their
-// hidden values.  A wave takes 16 RB rows (W = 1), or 16 shared by W waves.
+// Few outputs: columns 0 .. M - 1 of the product are W's rows, the next ones
+// the rows of as many of the tile's adapters' A as fit; the products go through
+// LDS, where each row's outputs take up their hidden values.  A wave takes 16 RB
+// rows (W = 1), or 16 shared by W waves.
 template <typename T, int RB, int NB, int W>
 __global__ __launch_bounds__(W == 16 ? 1024 : 256) void project_narrow(ProjArgs a, T *y, int64_t ys, float *hidden)
 {
@@ -176,12 +182,14 @@ __global__ __launch_bounds__(W == 16 ? 1024 : 256) void project_narrow(ProjArgs 
     constexpr int PER = NW / W;
     const T *x = (const T *)a.x, *w = (const T *)a.w, *fa = (const T *)a.a, *fb = (const T *)a.b;
     const int M = a.M, r = a.r, n = a.n;
+    const int fit = n ? (NB * 16 - M) / r : 0;  // adapters a pass has columns for
     for (int64_t tile0 = (int64_t)blockIdx.x * PER; tile0 < tiles; tile0 += (int64_t)gridDim.x * PER) {
         const int64_t row0 = (tile0 + wave / W) * 16 * RB;
-        int id = -1;  // of row `lane` of the wave's; a bad one stands as "none" in the walk
+        int id = -1;  // of row `lane` of the wave's
         if (n && lane < 16 * RB && row0 + lane < a.rows) id = a.ids[row0 + lane];
         const bool bad = id >= n;
-        int group = lane < 16 * RB && row0 + lane < a.rows ? (bad || id < 0 ? 0 : id + 1) : -1;
+        int state = lane < 16 * RB && row0 + lane < a.rows ? 0 : 3;  // 0: to do, 1: this pass, 2: done, 3: no row
+        int slot = -1;  // the row's adapter among the pass's
         const T *row[RB];
 #pragma unroll
         for (int i = 0; i < RB; ++i) row[i] = x + clamp_row(row0 + i * 16 + q, a.rows) * a.xs;
@@ -189,19 +197,33 @@ __global__ __launch_bounds__(W == 16 ? 1024 : 256) void project_narrow(ProjArgs 
         const int run = W == 1 ? a.K : (a.K + W * S - 1) / (W * S) * S;
         const int c0 = std::min(a.K, wave % W * run), c1 = std::min(a.K, c0 + run);
         for (int last = -1;;) {
-            const int cur = next_adapter(group, last);  // 0: rows without an adapter, i + 1: adapter i
-            if (cur > n) break;
-            last = cur;
-            const T *ai = cur ? fa + (int64_t)(cur - 1) * r * a.K : nullptr;
+            // the next adapters that fit beside W's columns, and the rows they serve;
+            // rows without an adapter go with the first pass
             const T *col[NB];
             f4 acc[RB][NB];
+            int colslot[NB];
 #pragma unroll
             for (int j = 0; j < NB; ++j) {
                 const int c = j * 16 + q;
-                col[j] = c < M ? w + c * a.ws : ai && c < M + r ? ai + (int64_t)(c - M) * a.K : nullptr;
+                colslot[j] = c < M || !n ? -1 : (c - M) / r;
+                col[j] = c < M ? w + c * a.ws : nullptr;
 #pragma unroll
                 for (int i = 0; i < RB; ++i) acc[i][j] = f4{0.f, 0.f, 0.f, 0.f};
             }
+            if (state == 0 && (id < 0 || bad)) state = 1;
+            for (int s = 0; s < fit; ++s) {
+                const int cur = next_adapter(bad ? -1 : id, last);
+                if (cur >= n) break;
+                last = cur;
+                if (state == 0 && id == cur) {
+                    state = 1;
+                    slot = s;
+                }
+#pragma unroll
+                for (int j = 0; j < NB; ++j)
+                    if (colslot[j] == s) col[j] = fa + ((int64_t)cur * r + (j * 16 + q - M - s * r)) * a.K;
+            }
+            if (!__any(state == 1)) break;
             row_products<false, T, RB, NB>(row, col, 1, c0, c1, acc);
             if (W > 1) __syncthreads();
 #pragma unroll
@@ -212,8 +234,8 @@ __global__ __launch_bounds__(W == 16 ? 1024 : 256) void project_narrow(ProjArgs 
                     for (int e = 0; e < 4; ++e) part[wave][i * 16 + g * 4 + e][j * 16 + q] = acc[i][j][e];
             if (W > 1) {
                 __syncthreads();
-                for (int k = threadIdx.x; k < 16 * RB * (M + r); k += 64 * NW) {
-                    const int rr = k / (M + r), c = k - rr * (M + r);
+                for (int k = threadIdx.x; k < 16 * RB * NB * 16; k += 64 * NW) {
+                    const int rr = k / (NB * 16), c = k % (NB * 16);
                     float s = part[0][rr][c];
 #pragma unroll
                     for (int o = 1; o < W; ++o) s += part[o][rr][c];
@@ -224,32 +246,33 @@ __global__ __launch_bounds__(W == 16 ? 1024 : 256) void project_narrow(ProjArgs 
                 __builtin_amdgcn_wave_barrier();
             }
             const float(*sum)[P] = part[W > 1 ? 0 : wave];
-            const float sc = cur && a.scale ? a.scale[cur - 1] : 1.f;
             if (wave % W == 0) {
                 for (int k = lane; k < (16 * RB * M + 63) / 64 * 64; k += 64) {
                     const int rr = k / M, m = k - rr * M;
-                    const bool mine = __shfl(group, rr & 63) == cur && rr < 16 * RB;
-                    const bool none = __shfl((int)bad, rr & 63);
+                    const bool mine = __shfl(state, rr & 63) == 1 && rr < 16 * RB;
+                    const int i = __shfl(id, rr & 63), at = M + __shfl(slot, rr & 63) * r;
                     if (!mine) continue;
                     float v = sum[rr][m];
-                    if (cur) {
-                        const T *bi = fb + ((int64_t)(cur - 1) * M + m) * r;
+                    if (i >= 0 && i < n) {
+                        const T *bi = fb + ((int64_t)i * M + m) * r;
                         float z = 0.f;
-                        for (int j = 0; j < r; ++j) z = fmaf(sum[rr][M + j], to_f32(bi[j]), z);
-                        v = fmaf(z, sc, v);
+                        for (int j = 0; j < r; ++j) z = fmaf(sum[rr][at + j], to_f32(bi[j]), z);
+                        v = fmaf(z, a.scale ? a.scale[i] : 1.f, v);
                     }
                     if (a.bias) v += a.bias[m];
-                    store_as(y + (row0 + rr) * ys + m, none ? NAN : v);
+                    store_as(y + (row0 + rr) * ys + m, i >= n && n ? NAN : v);
                 }
                 if (hidden) {
                     for (int k = lane; k < (16 * RB * r + 63) / 64 * 64; k += 64) {
                         const int rr = k / r, j = k - rr * r;
-                        const bool mine = __shfl(group, rr & 63) == cur && rr < 16 * RB;
-                        const bool none = __shfl((int)bad, rr & 63);
-                        if (mine) hidden[(row0 + rr) * r + j] = none ? NAN : cur ? sum[rr][M + j] : 0.f;
+                        const bool mine = __shfl(state, rr & 63) == 1 && rr < 16 * RB;
+                        const int i = __shfl(id, rr & 63), at = M + __shfl(slot, rr & 63) * r;
+                        if (mine) hidden[(row0 + rr) * r + j] = i >= n ? NAN : i < 0 ? 0.f : sum[rr][at + j];
                     }
                 }
             }
+            if (state == 1) state = 2;
+            if (!__any(state == 0)) break;
             if (W == 1) __builtin_amdgcn_wave_barrier();
         }
         if (W > 1) __syncthreads();
@@ -279,18 +302,32 @@ struct FactorArgs {
     const T *b;     // both in one pass: [n][M][r]
 };
 
-// Four adjacent values of a row from column c on, 0 past its C columns.  QUADS
-// (C a multiple of four): always one load, from inside the row, without a
-// branch that would keep the next row's load waiting.
-template <bool QUADS, typename T>
+// Four adjacent values of a row from column c on, 0 past its C columns.  Rows of
+// four or more (LOAD 0: a multiple of four; 1: any): always one load, from
+// inside the row, moved into place, without a branch that would keep the next
+// row's load waiting.  LOAD 2: shorter rows.
+template <int LOAD, typename T>
 __device__ __forceinline__ void four(const T *v, int c, int C, bool have, float (&vv)[4])
 {
-    if (QUADS || c + 4 <= C) {
-        unpack<T, 4>(load_words<4 * sizeof(T)>(v + min(c, C - 4)), vv);
-        have &= c < C;
-    } else {
+    if constexpr (LOAD == 2) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) vv[e] = c + e < C ? to_f32(v[c + e]) : 0.f;
+    } else {
+        float w[4];
+        const int from = min(c, C - 4), move = c - from;
+        unpack<T, 4>(load_words<4 * sizeof(T)>(v + from), w);
+        if constexpr (LOAD == 1) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                float x = w[e];
+#pragma unroll
+                for (int k = 1; k < 4; ++k) x = move == k ? (e + k < 4 ? w[(e + k) & 3] : 0.f) : x;
+                w[e] = x;  // later e only look at later w
+            }
+        }
+        have &= c < C;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) vv[e] = w[e];
     }
 #pragma unroll
     for (int e = 0; e < 4; ++e) vv[e] = have ? vv[e] : 0.f;
@@ -329,7 +366,7 @@ __device__ __forceinline__ void store_sums(const FactorArgs<T> &a, const FactorJ
 template <int NB>
 constexpr int kGroups = NB == 1 ? 8 : NB == 2 ? 4 : 2;
 
-template <typename T, int NB, int WC, bool QUADS, int MB>
+template <typename T, int NB, int WC, int LOAD, int MB>
 __global__ __launch_bounds__(256) void factor_grad(FactorArgs<T> a)
 {
     constexpr bool FUSED = MB > 0;
@@ -377,7 +414,7 @@ __global__ __launch_bounds__(256) void factor_grad(FactorArgs<T> a)
                         gv[k] = to_f32(jb.v[row * jb.vs + std::min(q, M - 1)]);
                         gv[k] = have && q < M ? gv[k] : 0.f;
                     }
-                    four<QUADS>(job.v + row * job.vs, c0 + q * 4, C, have, vv[k]);
+                    four<LOAD>(job.v + row * job.vs, c0 + q * 4, C, have, vv[k]);
                 }
 #pragma unroll
                 for (int k = 0; k < G; ++k) {
@@ -525,13 +562,14 @@ hipError_t go_rank(const T *v, int64_t vs, int64_t rows, int C, const T *f, int 
                    const int *ids, float *t, hipStream_t s)
 {
     const int waves = axis_waves<T>(rows, C);
-    // The 64 sixteens of 1024 rows over the workgroups of an adapter: up to two
-    // each where there are few adapters, fewer workgroups where the rows spread
-    // over many (a workgroup without rows costs the look at their ids).
-    const int per = waves == 1 ? 4 : 1, most = (int)std::min<int64_t>(32, (rows + 15) / 16);
-    const int slots = std::max(1, std::min(most, std::max(4, 512 / n)) / per);
+    // The 64 sixteens of 1024 rows over several workgroups of an adapter where
+    // there are too few otherwise; a workgroup without rows costs the look at
+    // their ids (550,000 mixed rows of 13 adapters, eight each: 779 us).
+    const int64_t units = (rows + 1023) / 1024 * n;
+    const int64_t most = waves == 1 ? 8 : std::min<int64_t>(32, (rows + 15) / 16);
+    const int slots = (int)std::max<int64_t>(1, std::min<int64_t>(most, 4096 / units));
     const RankArgs<T> a{v, f, vs, rows, C, n, r, slots, scale, ids, t};
-    const dim3 grid(slots, (unsigned)std::min<int64_t>((rows + 1023) / 1024 * n, 65535));
+    const dim3 grid(slots, (unsigned)std::min<int64_t>(units, 65535));
     if (waves == 16) hipLaunchKernelGGL((rank_rows<T, NB, 16, TRANS>), grid, dim3(1024), 0, s, a);
     else if (waves == 4) hipLaunchKernelGGL((rank_rows<T, NB, 4, TRANS>), grid, dim3(256), 0, s, a);
     else hipLaunchKernelGGL((rank_rows<T, NB, 1, TRANS>), grid, dim3(256), 0, s, a);
@@ -566,7 +604,9 @@ template <typename T>
 hipError_t project(const ProjArgs &a, int dtype, T *y, int64_t ys, float *hidden, float *h, float *parts, hipStream_t s)
 {
     if (narrow(a)) {
-        const int cols = a.M + a.r;
+        // columns for four adapters, as rows in any order name them, but for no
+        // more than 32 where one needs no more
+        const int cols = std::max(a.M + a.r, std::min(32, a.M + a.r * std::min(a.n, 4)));
         if (cols <= 16) return go_narrow<T, 1>(a, y, ys, hidden, s);
         if (cols <= 32) return go_narrow<T, 2>(a, y, ys, hidden, s);
         return go_narrow<T, 4>(a, y, ys, hidden, s);
@@ -592,10 +632,10 @@ hipError_t go_factor(FactorArgs<T> &a, hipStream_t s)
 {
     for (FactorJob<T> &j : a.job) j.ctiles = (j.C + 64 * WC - 1) / (64 * WC);
     const dim3 grid(a.job[0].ctiles + (MB ? 0 : a.job[1].ctiles), (unsigned)std::min<int64_t>((int64_t)a.n * a.runs, 65535));
-    if (a.job[0].C % 4 == 0 && (MB || a.job[1].C % 4 == 0))
-        hipLaunchKernelGGL((factor_grad<T, NB, WC, true, MB>), grid, dim3(256), 0, s, a);
-    else
-        hipLaunchKernelGGL((factor_grad<T, NB, WC, false, MB>), grid, dim3(256), 0, s, a);
+    const int c0 = a.job[0].C, c1 = MB ? c0 : a.job[1].C;
+    if (std::min(c0, c1) < 4) hipLaunchKernelGGL((factor_grad<T, NB, WC, 2, MB>), grid, dim3(256), 0, s, a);
+    else if (c0 % 4 || c1 % 4) hipLaunchKernelGGL((factor_grad<T, NB, WC, 1, MB>), grid, dim3(256), 0, s, a);
+    else hipLaunchKernelGGL((factor_grad<T, NB, WC, 0, MB>), grid, dim3(256), 0, s, a);
     return hipGetLastError();
 }
 
