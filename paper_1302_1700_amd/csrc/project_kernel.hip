@@ -295,8 +295,8 @@ struct FactorJob {
 template <typename T>
 struct FactorArgs {
     FactorJob<T> job[2];
-    int64_t rows;
-    int run_rows, runs, n, r;
+    int64_t rows, run_rows;
+    int runs, n, r;
     const int *ids;
     uint8_t *used;  // [n][runs]: the run holds rows of the adapter
     const T *b;     // both in one pass: [n][M][r]
@@ -381,7 +381,7 @@ __global__ __launch_bounds__(256) void factor_grad(FactorArgs<T> a)
     const bool second = FUSED && blockIdx.x == 0 && wave % WC == 0;  // this wave also makes the other factor's
     for (int64_t unit = blockIdx.y; unit < (int64_t)a.n * a.runs; unit += gridDim.y) {
         const int i = (int)(unit / a.runs), run = (int)(unit - (int64_t)i * a.runs);
-        const int64_t begin = (int64_t)run * a.run_rows, end = std::min(a.rows, begin + a.run_rows);
+        const int64_t begin = run * a.run_rows, end = std::min(a.rows, begin + a.run_rows);
         float bi[FUSED ? MB : 1];
         if constexpr (FUSED) {
             const float sc = jb.scale ? jb.scale[i] : 1.f;
@@ -535,7 +535,8 @@ int axis_waves(int64_t rows, int C)
 bool both(const ProjArgs &a) { return a.M <= 16 && a.r <= 16; }
 
 struct RunPlan {
-    int run_rows, runs;
+    int64_t run_rows;
+    int runs;
     size_t parts[2], used;  // bytes
 };
 
@@ -548,8 +549,7 @@ RunPlan run_plan(const ProjArgs &a)
     int64_t runs = std::max<int64_t>(1, std::min<int64_t>(2048 / ctiles, a.rows / 128));
     runs = std::max<int64_t>(1, std::min<int64_t>(runs, (int64_t)(268435456.0 / part)));
     RunPlan p;
-    p.run_rows = (int)(((a.rows + runs - 1) / runs + 63) / 64 * 64);
-    p.run_rows = std::max(p.run_rows, 64);
+    p.run_rows = std::max<int64_t>(64, ((a.rows + runs - 1) / runs + 63) / 64 * 64);
     p.runs = (int)std::max<int64_t>(1, (a.rows + p.run_rows - 1) / p.run_rows);
     p.parts[0] = p.runs > 1 ? up256((size_t)a.n * p.runs * a.r * a.K * sizeof(float)) : 0;
     p.parts[1] = p.runs > 1 ? up256((size_t)a.n * p.runs * a.r * a.M * sizeof(float)) : 0;

@@ -91,23 +91,29 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void project_tiles(WideArgs a, int
     constexpr int RPB = BN / E;  // pieces of a row of W as in memory
     const T *va = reinterpret_cast<const T *>(a.v) + m0 * a.vs + c_begin;
     const T *wb = reinterpret_cast<const T *>(a.w) + (TRANS ? (int64_t)c_begin * a.ws + n0 : (int64_t)n0 * a.ws + c_begin);
-    uint32_t pa[PA], pb[PB];  // a thread's places from there, in bytes
+    // Large tiles: buffer loads, whose addresses are one register a piece and a
+    // scalar that moves along (as pointers they took two each and spilled).
+    // The host sends only 16-byte aligned rows of less than 2^31 bytes a tile, and
+    // whole steps.  Smaller tiles: any row stride.
+    constexpr bool BUFFER = !AHEAD;
+    using Place = typename std::conditional<BUFFER, uint32_t, int64_t>::type;
+    Place pa[PA], pb[PB];  // a thread's places from there, in bytes
 #pragma unroll
     for (int i = 0; i < PA; ++i)
-        pa[i] = (uint32_t)(((clamp_row(m0 + i * RT + (threadIdx.x >> 3), a.rows) - m0) * a.vs + (threadIdx.x & 7) * E) * sizeof(T));
+        pa[i] = (Place)(((clamp_row(m0 + i * RT + (threadIdx.x >> 3), a.rows) - m0) * a.vs + (threadIdx.x & 7) * E) * sizeof(T));
 #pragma unroll
     for (int i = 0; i < PB; ++i) {
         const int piece = i * NT + threadIdx.x;
         if constexpr (TRANS) {
             int col = piece % RPB * E;
             if (a.cols % E == 0) col = min(n0 + col, a.cols - E) - n0;  // whole pieces lie inside or outside
-            pb[i] = (uint32_t)((piece / RPB * a.ws + col) * sizeof(T));
+            pb[i] = (Place)((piece / RPB * a.ws + col) * sizeof(T));
         } else {
-            pb[i] = (uint32_t)(((min(n0 + i * RT + (int)(threadIdx.x >> 3), a.cols - 1) - n0) * a.ws + (threadIdx.x & 7) * E) *
+            pb[i] = (Place)(((min(n0 + i * RT + (int)(threadIdx.x >> 3), a.cols - 1) - n0) * a.ws + (threadIdx.x & 7) * E) *
                                sizeof(T));
         }
     }
-    const auto place = [](const T *base, uint32_t bytes) {
+    const auto place = [](const T *base, Place bytes) {
         return reinterpret_cast<const T *>(reinterpret_cast<const char *>(base) + bytes);
     };
     // steps are fetched in their order: the bases move along
@@ -117,11 +123,6 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void project_tiles(WideArgs a, int
         va += D;
         wb += TRANS ? D * a.ws : D;
     };
-    // Large tiles: buffer loads, whose addresses are one register a piece and a
-    // scalar that moves along (as pointers they took two each and spilled).
-    // The host sends only 16-byte aligned rows of less than 2^31 bytes a tile, and
-    // whole steps.
-    constexpr bool BUFFER = !AHEAD;
     const __amdgpu_buffer_rsrc_t buf_a = __builtin_amdgcn_make_buffer_rsrc((void *)va, 0, 0x7fffffff, 0x00020000);
     const __amdgpu_buffer_rsrc_t buf_b = __builtin_amdgcn_make_buffer_rsrc((void *)wb, 0, 0x7fffffff, 0x00020000);
     int move_a = 0, move_b = 0;

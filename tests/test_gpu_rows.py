@@ -325,6 +325,48 @@ def test_project_keeps_infinities_to_their_rows(fsb):
         assert not torch.isfinite(y[hit]).all(1).any()
 
 
+# Every tile size, and each way to share the work: tiles of 128 and 256 rows and columns with whole and cut steps,
+# sixteen waves to a few rows, waves that share rows of few columns, rows enough for a wave to two sixteens of them.
+LARGE = [
+    (2100, 100, 2000, 16, 5, "mixed"), (2051, 2004, 70, 3, 3, "bad"), (3500, 128, 3600, 16, 5, "bad"),
+    (3333, 3608, 128, 9, 4, "runs"), (3330, 3600, 64, 40, 2, "mixed"), (40, 1200, 40, 8, 3, "mixed"),
+    (50, 40, 60, 128, 3, "mixed"), (70, 33, 50, 40, 2, "mixed"), (90, 100, 70, 20, 3, "bad"), (300, 3, 2, 1, 2, "mixed"),
+    (70001, 40, 3, 5, 3, "bad"), (66000, 24, 30, 34, 4, "mixed")]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("N,K,M,r,n,ids", LARGE)
+def test_project_large(fsb, dtype, N, K, M, r, n, ids):
+    test_project(fsb, dtype, N, K, M, r, n, ids)
+    test_project_grad(fsb, dtype, N, K, M, r, n, ids)
+
+
+def test_no_rows_leave_zero_gradients(fsb):
+    for dt in (torch.float32, torch.bfloat16):
+        for K, M, r in ((20, 2, 4), (20, 30, 40)):
+            e = lambda *s: torch.ones(s, dtype=dt, device="cuda")
+            ids = torch.zeros(0, dtype=torch.int32, device="cuda")
+            gx, ga, gb = fsb.project_grad(e(0, M), e(0, K), e(M, K), fsb.Adapters(e(3, r, K), e(3, M, r)), ids)
+            assert gx.shape == (0, K) and (ga == 0).all() and (gb == 0).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_project_far_rows(fsb, dtype):
+    """Rows, gradients and outputs whose elements lie beyond 2^31 from the first."""
+    gen = torch.Generator(device="cuda").manual_seed(6)
+    rnd = lambda *s: torch.randn(s, generator=gen, device="cuda").to(DT[dtype])
+    stride = (1 << 29) + 8
+    for K, M, r in ((72, 9, 3), (96, 136, 16)):
+        x, w, g, ad = rnd(6, K), rnd(M, K), rnd(6, M), fsb.Adapters(rnd(2, r, K), rnd(2, M, r))
+        ids = torch.tensor([0, 1, -1, 1, 0, 1], dtype=torch.int32, device="cuda")
+        store = torch.empty(5 * stride + 512, dtype=DT[dtype], device="cuda")
+        far = lambda t, at: store[at:].as_strided(t.shape, (stride, 1)).copy_(t)
+        fx, fg, out = far(x, 0), far(g, 128), store[300:].as_strided((6, M), (stride, 1))
+        assert torch.equal(fsb.project(fx, w, None, ad, ids, out=out), fsb.project(x, w, None, ad, ids))
+        for a, b in zip(fsb.project_grad(fg, fx, w, ad, ids), fsb.project_grad(g, x, w, ad, ids)):
+            assert torch.equal(a, b)
+
+
 # -- streams, graphs, the operators together --------------------------------------------
 def test_on_another_stream_and_captured(fsb):
     """The four calls on a side stream, then captured once and replayed on new inputs, between the program's own work."""
