@@ -546,7 +546,8 @@ RunPlan run_plan(const ProjArgs &a)
 {
     const int64_t ctiles = both(a) ? (a.K + 255) / 256 : (a.K + 255) / 256 + (a.M + 255) / 256;
     const double part = (double)a.n * a.r * (a.K + a.M) * sizeof(float);
-    int64_t runs = std::max<int64_t>(1, std::min<int64_t>(2048 / ctiles, a.rows / 128));
+    // below 512 rows a launch to join them costs more than the runs save
+    int64_t runs = a.rows < 512 ? 1 : std::max<int64_t>(1, std::min<int64_t>(2048 / ctiles, a.rows / 128));
     runs = std::max<int64_t>(1, std::min<int64_t>(runs, (int64_t)(268435456.0 / part)));
     RunPlan p;
     p.run_rows = std::max<int64_t>(64, ((a.rows + runs - 1) / runs + 63) / 64 * 64);

@@ -326,9 +326,13 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void project_tiles(WideArgs a, int
             put((s + 1) & 1);
             fetch();
             read(s & 1, 0, oa, ob);
+            __builtin_amdgcn_s_setprio(1);
             products(oa, ob);
+            __builtin_amdgcn_s_setprio(0);
             read(s & 1, 1, oa, ob);
+            __builtin_amdgcn_s_setprio(1);
             products(oa, ob);
+            __builtin_amdgcn_s_setprio(0);
             __syncthreads();
         }
     }
@@ -390,16 +394,17 @@ __global__ __launch_bounds__(256) void project_join(WideArgs a, int splits)
     for (int64_t k = (int64_t)blockIdx.x * 256 + threadIdx.x; k < total; k += (int64_t)gridDim.x * 256) {
         const int64_t row = k / quads;
         const int col = (int)(k - row * quads) * 4, have = min(4, a.cols - col);
+        const int id = a.n ? a.ids[row] : -1;
         float y[4] = {0.f, 0.f, 0.f, 0.f}, z[4] = {0.f, 0.f, 0.f, 0.f};
+        // four columns from inside the row, moved into place where the row ends
+        const int from = min(col, max(a.cols - 4, 0)), move = col - from;
         for (int s0 = 0; s0 < splits; s0 += 8) {
             float v[8][4];  // in flight together
 #pragma unroll
             for (int s = 0; s < 8; ++s) {
                 const float *p = a.parts + ((int64_t)min(s0 + s, splits - 1) * a.rows + row) * a.cols;
-                if (a.cols >= 4) {
-                    // the last columns from further left, moved into place below
-                    unpack<float, 4>(load_words<16>(p + min(col, a.cols - 4)), v[s]);
-                } else {
+                if (a.cols >= 4) unpack<float, 4>(load_words<16>(p + from), v[s]);
+                else {
 #pragma unroll
                     for (int e = 0; e < 4; ++e) v[s][e] = e < have ? p[col + e] : 0.f;
                 }
@@ -409,30 +414,35 @@ __global__ __launch_bounds__(256) void project_join(WideArgs a, int splits)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) y[e] += s0 + s < splits ? v[s][e] : 0.f;
         }
-        if (have < 4 && a.cols >= 4) {
-            const int move = 4 - have;
+        if (move) {
 #pragma unroll
-            for (int e = 0; e < 3; ++e) y[e] = e + move < 4 ? (move == 1 ? y[e + 1] : move == 2 ? y[(e + 2) & 3] : y[3]) : 0.f;
+            for (int e = 0; e < 3; ++e) y[e] = move == 1 ? y[e + 1] : move == 2 ? y[(e + 2) & 3] : y[3];
         }
-        const int id = a.n ? a.ids[row] : -1;
         if (id >= 0 && id < a.n) {
             const T *f = reinterpret_cast<const T *>(a.f) + (int64_t)id * a.cols * a.r;
             const float *t = a.t + row * a.r;
             if constexpr (TRANS) {
+#pragma unroll 4
                 for (int j = 0; j < a.r; ++j)
 #pragma unroll
                     for (int e = 0; e < 4; ++e)
-                        if (e < have) z[e] = fmaf(t[j], to_f32(f[(int64_t)j * a.cols + col + e]), z[e]);
+                        z[e] = fmaf(t[j], to_f32(f[(int64_t)j * a.cols + min(col + e, a.cols - 1)]), z[e]);
             } else {
+                const bool whole = a.r % E == 0;
+                for (int j = 0; j < a.r; j += E) {
+                    Operand<T> o[4];  // of the four columns, in flight together
+                    float tv[E];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    if (e >= have) continue;
-                    for (int j = 0; j < a.r; j += E) {
-                        const Operand<T> o = load_operand(f + (int64_t)(col + e) * a.r + j, a.r - j);
+                    for (int e = 0; e < 4; ++e)
+                        o[e] = load_operand(f + (int64_t)min(col + e, a.cols - 1) * a.r + j, whole ? E : a.r - j);
 #pragma unroll
-                        for (int p = 0; p < E; ++p)
-                            if (j + p < a.r) z[e] = fmaf(t[j + p], to_f32((T)o.v[p]), z[e]);
-                    }
+                    for (int p = 0; p < E; ++p) tv[p] = t[min(j + p, a.r - 1)];
+#pragma unroll
+                    for (int p = 0; p < E; ++p)
+                        if (whole || j + p < a.r) {
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) z[e] = fmaf(tv[p], to_f32((T)o[e].v[p]), z[e]);
+                        }
                 }
             }
             const float sc = !TRANS && a.scale ? a.scale[id] : 1.f;
