@@ -103,9 +103,9 @@ struct RankArgs {
 };
 
 template <typename T, int NB, int W, bool TRANS>
-__global__ __launch_bounds__(W == 16 ? 1024 : 256) void rank_rows(RankArgs<T> a)
+__global__ __launch_bounds__(W > 4 ? 64 * W : 256) void rank_rows(RankArgs<T> a)
 {
-    constexpr int NW = W == 16 ? 16 : 4, PER = NW / W, RB = W == 1 ? 2 : 1;  // RB sixteens of rows to a product
+    constexpr int NW = W > 4 ? W : 4, PER = NW / W, RB = W == 1 ? 2 : 1;  // RB sixteens of rows to a product
     __shared__ float part[W > 1 ? W * 256 : 1];
     __shared__ int list[1024], count[16];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, q = lane & 15, g = lane >> 4;
@@ -173,9 +173,9 @@ __global__ __launch_bounds__(W == 16 ? 1024 : 256) void rank_rows(RankArgs<T> a)
 // LDS, where each row's outputs take up their hidden values.  A wave takes 16 RB
 // rows (W = 1), or 16 shared by W waves.
 template <typename T, int RB, int NB, int W>
-__global__ __launch_bounds__(W == 16 ? 1024 : 256) void project_narrow(ProjArgs a, T *y, int64_t ys, float *hidden)
+__global__ __launch_bounds__(W > 4 ? 64 * W : 256) void project_narrow(ProjArgs a, T *y, int64_t ys, float *hidden)
 {
-    constexpr int P = NB * 16 + 1, NW = W == 16 ? 16 : 4;
+    constexpr int P = NB * 16 + 1, NW = W > 4 ? W : 4;
     __shared__ float part[NW][16 * RB][P];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, q = lane & 15, g = lane >> 4;
     const int64_t tiles = (a.rows + 16 * RB - 1) / (16 * RB);
@@ -523,12 +523,12 @@ size_t rank_bytes(const ProjArgs &a) { return up256((size_t)a.rows * a.r * sizeo
 bool narrow(const ProjArgs &a) { return a.M + a.r <= 64; }
 
 // Waves that share the summed axis of a product: four while whole waves to one
-// would leave CUs idle, sixteen for a handful.  The same rule wherever rows meet
+// would leave CUs idle, eight or sixteen for fewer.  The same rule wherever rows meet
 // A: the hidden rows then have the same bits from every kernel.
 template <typename T>
 int axis_waves(int64_t rows, int C)
 {
-    if (rows <= 8192 && C >= 32 * kStep<T>) return 16;
+    if (rows <= 8192 && C >= 32 * kStep<T>) return rows <= 256 ? 16 : 8;
     return rows <= 16 * 4096 && C >= 8 * kStep<T> ? 4 : 1;
 }
 
@@ -567,11 +567,12 @@ hipError_t go_rank(const T *v, int64_t vs, int64_t rows, int C, const T *f, int 
     // there are too few otherwise; a workgroup without rows costs the look at
     // their ids (550,000 mixed rows of 13 adapters, eight each: 779 us).
     const int64_t units = (rows + 1023) / 1024 * n;
-    const int64_t most = waves == 1 ? 8 : std::min<int64_t>(32, (rows + 15) / 16);
+    const int64_t most = waves == 1 ? 8 : std::min<int64_t>(64, (rows + 15) / 16);
     const int slots = (int)std::max<int64_t>(1, std::min<int64_t>(most, 4096 / units));
     const RankArgs<T> a{v, f, vs, rows, C, n, r, slots, scale, ids, t};
     const dim3 grid(slots, (unsigned)std::min<int64_t>(units, 65535));
     if (waves == 16) hipLaunchKernelGGL((rank_rows<T, NB, 16, TRANS>), grid, dim3(1024), 0, s, a);
+    else if (waves == 8) hipLaunchKernelGGL((rank_rows<T, NB, 8, TRANS>), grid, dim3(512), 0, s, a);
     else if (waves == 4) hipLaunchKernelGGL((rank_rows<T, NB, 4, TRANS>), grid, dim3(256), 0, s, a);
     else hipLaunchKernelGGL((rank_rows<T, NB, 1, TRANS>), grid, dim3(256), 0, s, a);
     return hipGetLastError();
@@ -594,6 +595,8 @@ hipError_t go_narrow(const ProjArgs &a, T *y, int64_t ys, float *hidden, hipStre
     const int waves = axis_waves<T>(a.rows, a.K);
     if (waves == 16)
         hipLaunchKernelGGL((project_narrow<T, 1, NB, 16>), dim3(grid_of(tiles)), dim3(1024), 0, s, a, y, ys, hidden);
+    else if (waves == 8)
+        hipLaunchKernelGGL((project_narrow<T, 1, NB, 8>), dim3(grid_of(tiles)), dim3(512), 0, s, a, y, ys, hidden);
     else if (waves == 4)
         hipLaunchKernelGGL((project_narrow<T, 1, NB, 4>), dim3(grid_of(tiles)), dim3(256), 0, s, a, y, ys, hidden);
     else
