@@ -416,6 +416,8 @@ def _row_out(t, name, like, shape):
     """A given or new output of rows, and its row stride."""
     import torch
     if t is None:
+        if shape == like.shape and like.is_contiguous():
+            return torch.empty_like(like), shape[-1]
         return torch.empty(shape, dtype=like.dtype, device=like.device), shape[-1]
     if t.dtype != like.dtype or tuple(t.shape) != tuple(shape) or t.device != like.device:
         raise ValueError("%s must be a %s tensor %s on %s" % (name, str(like.dtype)[6:], tuple(shape), like.device))
@@ -492,11 +494,11 @@ def logprobs(scores, labels=None, n_top=0, temperature=1.0, workspace=None, stre
     _check(lib.fs_logprobs_workspace(rows, V, dt, n_top, ctypes.byref(need)), lib)
     ws, have = _row_workspace(need.value, workspace, dev)
     f32 = torch.float32
-    logp = torch.empty(shape, dtype=f32, device=dev) if labels is not None else None
     entropy = torch.empty(shape, dtype=f32, device=dev)
+    logp = torch.empty_like(entropy) if labels is not None else None
     norm = torch.empty((*shape, 2), dtype=f32, device=dev)
-    top_id = torch.empty((*shape, n_top), dtype=torch.int32, device=dev) if n_top else None
     top_logp = torch.empty((*shape, n_top), dtype=f32, device=dev) if n_top else None
+    top_id = torch.empty_like(top_logp, dtype=torch.int32) if n_top else None
     _check(lib.fs_logprobs(scores.data_ptr(), rows, V, row_stride, dt, float(temperature), _ptr(labels), n_top,
                            _ptr(logp), entropy.data_ptr(), norm.data_ptr(), _ptr(top_id), _ptr(top_logp),
                            _ptr(ws), have, _current_stream(dev)), lib)

@@ -331,7 +331,10 @@ LARGE = [
     (2100, 100, 2000, 16, 5, "mixed"), (2051, 2004, 70, 3, 3, "bad"), (3500, 128, 3600, 16, 5, "bad"),
     (3333, 3608, 128, 9, 4, "runs"), (3330, 3600, 64, 40, 2, "mixed"), (40, 1200, 40, 8, 3, "mixed"),
     (50, 40, 60, 128, 3, "mixed"), (70, 33, 50, 40, 2, "mixed"), (90, 100, 70, 20, 3, "bad"), (300, 3, 2, 1, 2, "mixed"),
-    (70001, 40, 3, 5, 3, "bad"), (66000, 24, 30, 34, 4, "mixed")]
+    (70001, 40, 3, 5, 3, "bad"), (66000, 24, 30, 34, 4, "mixed"),
+    # more adapters than rows, more than 1024 of them; a few adapters over several thousand rows
+    (40, 70, 90, 3, 1500, "mixed"), (2500, 48, 80, 2, 1100, "bad"), (37, 1100, 90, 20, 1025, "bad"),
+    (3000, 1030, 100, 4, 3, "mixed"), (1025, 520, 100, 4, 1024, "mixed")]
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
