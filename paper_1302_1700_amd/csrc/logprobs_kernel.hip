@@ -587,23 +587,28 @@ __global__ __launch_bounds__(256) void logprobs_grad_long(LogprobGradArgs a, int
 int capped(int64_t blocks) { return (int)std::max<int64_t>(1, std::min<int64_t>(blocks, 1 << 22)); }
 
 // -- choices -------------------------------------------------------------------
-constexpr int kShort = 512;  // classes a wave's registers hold at 8 a lane
+// Classes a wave's registers hold at 8 a lane.  20,000 x 500 float32: 11 us, as
+// long rows of four waves 51; the 5 best 32 and 133.
+constexpr int kShort = 512;
 
 struct LongPlan {
     int waves, splits, per_split;
 };
 
-constexpr int kBatch = 4;  // chunks of a batch; 2 where sixteen waves share a row
+constexpr int kBatch = 4;  // chunks of a batch
 
+// One wave to a row where its share of the row's fixed costs weighs more than
+// the wait for it: 4000 x 8192 bf16, 5 best: 22 us, with four waves 37; 4000 x
+// 32768: 65 and 57.  Where rows are few and long, runs of eight batches joined by
+// a second launch (4 x 131072 float32, 5 best: 15.5 us, whole 22.6; shorter ones
+// do not repay it: 64 x 16384 float32 12 us, whole 8.7).
 LongPlan long_plan(int64_t rows, int V, int dtype)
 {
     const int batch = kBatch * 64 * (dtype == DT_BF16 ? 8 : 4);
-    LongPlan p{V <= 2 * batch ? 1 : 4, 1, V};
-    if (rows <= 512 && V > 2 * batch) {
-        p.waves = 16;
-        // runs of two batches a wave, while there are CUs left to take them
+    LongPlan p{V <= 2 * batch || (rows > 512 && V <= 8192) ? 1 : 4, 1, V};
+    if (rows <= 512 && V > 24 * batch) {
         const int most = (int)std::min<int64_t>(64, std::max<int64_t>(1, 512 / rows));
-        p.splits = std::min(most, (V + 16 * batch - 1) / (16 * batch));
+        p.splits = std::min(most, (V + 8 * batch - 1) / (8 * batch));
         if (p.splits > 1) {
             p.per_split = ((V + p.splits - 1) / p.splits + 7) / 8 * 8;
             p.splits = (V + p.per_split - 1) / p.per_split;
@@ -648,8 +653,7 @@ hipError_t run(const LogprobArgs &a, int dtype, char *parts, hipStream_t s)
     if (V <= kShort) return go_short<T, 64, C, N>(a, s);
     const LongPlan p = long_plan(a.rows, V, dtype);
     if (p.waves == 1) return go_long<T, 1, kBatch>(a, p, parts, s);
-    if (p.waves == 4) return go_long<T, 4, kBatch>(a, p, parts, s);
-    return go_long<T, 16, 2>(a, p, parts, s);
+    return go_long<T, 4, kBatch>(a, p, parts, s);
 }
 
 template <typename T, int G, int N>

@@ -520,18 +520,26 @@ __global__ __launch_bounds__(256) void factor_join(FactorArgs<T> a)
 // -- choices and workspace ---------------------------------------------------------
 size_t up256(size_t v) { return (v + 255) & ~(size_t)255; }
 size_t rank_bytes(const ProjArgs &a) { return up256((size_t)a.rows * a.r * sizeof(float)); }
+
+// W's and A's rows as columns of one product: 1M x 200 -> 20 float32, rank 8: 488
+// us, rows times A first and tiles of 64 columns then 805.
 bool narrow(const ProjArgs &a) { return a.M + a.r <= 64; }
 
-// Waves that share the summed axis of a product: four while whole waves to one
-// would leave CUs idle, eight or sixteen for fewer.  The same rule wherever rows meet
-// A: the hidden rows then have the same bits from every kernel.
+// Waves that share the summed axis of a product: the fewer rows and the longer
+// the axis, the more (bf16, 20 outputs, rank 8: 2048 x 4096 with eight 19 us, with
+// four 40, with one 65; 20,000 x 4096 with four 63, with one 103; 40,000 x 1024
+// with four 48, with one 43).  The same rule wherever rows meet A: the hidden
+// rows then have the same bits from every kernel.
 template <typename T>
 int axis_waves(int64_t rows, int C)
 {
-    if (rows <= 8192 && C >= 32 * kStep<T>) return rows <= 256 ? 16 : 8;
-    return rows <= 16 * 4096 && C >= 8 * kStep<T> ? 4 : 1;
+    const int steps = C / kStep<T>;
+    if (rows <= 8192 && steps >= 32) return rows <= 256 ? 16 : 8;
+    return steps >= 8 && rows <= (steps >= 64 ? 65536 : 16384) ? 4 : 1;
 }
 
+// Both factors' gradients in one pass: 1M x 200 -> 2 float32, rank 4: 247 us, with
+// the ranks' rows through memory and two passes 548.
 bool both(const ProjArgs &a) { return a.M <= 16 && a.r <= 16; }
 
 struct RunPlan {
