@@ -92,6 +92,33 @@ def test_logprobs(fsb, dtype, rows, V, n_top, kind):
     ro.close(_np(r.entropy), ent, terms + log_s[:, 0], "entropy")
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("V", [600, 8192, 50000, 131072])
+@pytest.mark.parametrize("rows", [2, 700])
+def test_best_classes_in_few_hands(fsb, dtype, V, rows):
+    """Rows of one value, and rows whose best classes all lie where one thread reads (16 bytes of every 1024): equal
+    ones, and more of them than a list holds."""
+    n, period, width = 64, 1024 // (4 if dtype == "f32" else 2), 4 if dtype == "f32" else 8
+    x = torch.zeros((rows, V), dtype=DT[dtype], device="cuda")
+    j = torch.arange(V, device="cuda")
+    few = (j % period) < width
+    x[1::2, few] = 3.0
+    if rows > 2:
+        x[3::2, few] = (j[few] * 37 % 101).to(DT[dtype])
+        x[2] = -float("inf")
+        x[2, V - 1] = 1.0
+    print("few hands", dtype, V, rows, flush=True)
+    r = fsb.logprobs(x, n_top=n)
+    torch.cuda.synchronize()
+    want = x[:4].float().cpu().sort(stable=True, dim=1, descending=True)
+    ids = want.indices[:, :n].int()
+    ids[want.values[:, :n] == -float("inf")] = -1
+    assert torch.equal(r.top_id[:4].cpu(), ids)
+    assert torch.equal(r.top_id[0::2][2:], r.top_id[:1].expand_as(r.top_id[0::2][2:]))
+    if rows > 4:
+        assert torch.equal(r.top_id[3::2], r.top_id[3:4].expand_as(r.top_id[3::2]))
+
+
 @pytest.mark.parametrize("kind", ["plain", "peaks", "masked", "far"])
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("rows,V", [(1, 1), (1000, 2), (333, 4), (65, 7), (130, 10), (41, 64), (33, 65), (17, 513),
@@ -407,6 +434,33 @@ def test_on_another_stream_and_captured(fsb):
         torch.cuda.synchronize()
         for g, w in zip(held, want):
             assert torch.equal(g, w)
+
+
+def test_two_streams_at_once(fsb):
+    """The same calls side by side on two streams give what each gives alone."""
+    d = [_cuda(_problem(31 + k, "bf16", 900, 512, 300, 8, 5, "mixed")) for k in range(2)]
+    ads = [_adapters(fsb, c) for c in d]
+    x = [torch.randn((40, 60000), device="cuda", generator=torch.Generator(device="cuda").manual_seed(k)) for k in range(2)]
+
+    def calls(k):
+        y, h = fsb.project(d[k]["x"], d[k]["w"], d[k]["bias"], ads[k], d[k]["ids"], return_hidden=True)
+        g = fsb.project_grad(d[k]["g"], d[k]["x"], d[k]["w"], ads[k], d[k]["ids"], hidden=h)
+        r = fsb.logprobs(x[k], n_top=9)
+        return (y, h, *g, r.entropy, r.norm, r.top_id, r.top_logp)
+
+    want = [calls(k) for k in range(2)]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    got = [[], []]
+    for _ in range(3):
+        for k in range(2):
+            with torch.cuda.stream(streams[k]):
+                got[k].append(calls(k))
+    torch.cuda.synchronize()
+    for k in range(2):
+        for result in got[k]:
+            for a, b in zip(result, want[k]):
+                assert torch.equal(a, b)
 
 
 def test_adapter_of_a_net_s_last_layer(fsb):
