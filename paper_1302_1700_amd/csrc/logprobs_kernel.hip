@@ -19,7 +19,9 @@ namespace fs {
 namespace {
 
 constexpr float kLowest = -3.402823466e38f;
-constexpr float kLog2e = 1.44269504088896f, kLn2 = 0.693147180559945f;
+constexpr double kLog2eExact = 1.4426950408889634;  // log2(e) = 1 / ln 2, to 53 bits
+constexpr float kLog2e = (float)kLog2eExact, kLn2 = 0.693147180559945f;
+constexpr float kLog2eRest = (float)(kLog2eExact - (double)kLog2e);  // what float32 leaves of it
 constexpr float kFar = -1e30f;
 
 // Elements per 16-byte load: rows start anywhere their element type may.
@@ -498,14 +500,18 @@ __global__ __launch_bounds__(256) void logprobs_join(LogprobArgs a, int splits, 
 }
 
 // -- gradient ------------------------------------------------------------------
-// exp with the product's rounding put back: p is off by its own rounding, not
-// by |ln p| times it
+// e^x = 2^(x log2 e) = 2^t 2^r for any t + r = x log2 e.  t is the product as
+// float32 rounds it and r what that leaves: the product's own error, which a
+// fused multiply-add gives exactly (Ogita, Rump, Oishi 2005, TwoProductFMA), plus x
+// times what float32 leaves of log2 e.  |r| is below 2^-15 at |x| <= 200, so
+// 2^r is 1 + r ln 2, the first terms of its series, to 2^-31.  The result is
+// off by its own roundings, not by |x| times them as exp2 of t alone is.
 __device__ __forceinline__ float exp_exact(float x)
 {
-    const float t = fmaxf(x, -200.f) * kLog2e;
-    const float rest = fmaf(fmaxf(x, -200.f), kLog2e, -t) + fmaxf(x, -200.f) * 1.925963033e-8f;
+    const float y = fmaxf(x, -200.f), t = y * kLog2e;
+    const float r = fmaf(y, kLog2e, -t) + y * kLog2eRest;
     const float e = __builtin_amdgcn_exp2f(t);
-    return x != x ? x : fmaf(e, rest * kLn2, e);
+    return x != x ? x : fmaf(e, r * kLn2, e);
 }
 
 // What the elements of a row's gradient share.
