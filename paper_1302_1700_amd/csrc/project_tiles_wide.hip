@@ -215,6 +215,8 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void project_tiles(WideArgs a, int
                     const int col = min(n0 + wn + j * 16 + q, a.cols - 1);
                     of[j] = TRANS ? gather_operand(f + (int64_t)at * a.cols + col, a.cols, have)
                                   : load_operand(f + (int64_t)col * a.r + at, have);
+                    // past the rank both operands are 0: 0 times an infinity is none
+                    if (even) of[j].v = k < a.r ? of[j].v : decltype(of[j].v){};
                 }
 #pragma unroll
                 for (int h = 0; h < WM; h += H) {

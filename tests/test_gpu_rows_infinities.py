@@ -1,0 +1,60 @@
+"""Infinite and very large values in the projection and its gradient: what the definition says of them, from every
+kernel that the sizes may select."""
+import numpy as np
+import pytest
+
+import rows_oracle as ro
+from test_gpu_rows import DT, _absolute, _adapters, _check, _cuda, _f64, _problem, fsb  # noqa: F401
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+# rows, inputs, outputs, rank, adapters of the forward pass; for the rows' gradient inputs and outputs change places
+FEW = [(70, 48, 40, 4, 3), (70, 48, 40, 8, 3)]                 # one pass over the rows
+TILES = [(70, 48, 100, 3, 3), (70, 48, 100, 4, 3), (70, 48, 100, 8, 3), (70, 48, 100, 12, 3), (70, 48, 100, 24, 3),
+         (70, 48, 100, 40, 2), (2051, 40, 2004, 4, 3), (2051, 40, 2004, 8, 3), (3500, 128, 3600, 16, 3)]
+SPLIT = [(40, 1200, 100, 8, 3)]                                 # the summed axis in stretches
+KEYS, GRAD_KEYS = ("x", "w", "bias", "a", "b", "scale", "ids"), ("g", "x", "w", "a", "b", "scale", "ids")
+
+
+def _forward(fsb, d, dtype):
+    """project against the definition: infinities of the same sign, NaN where it has them, the rest within bounds."""
+    c, o = _cuda(d), _f64(d)
+    K, r = d["x"].shape[1], d["a"].shape[1]
+    y, h = fsb.project(c["x"], c["w"], c["bias"], _adapters(fsb, c), c["ids"], return_hidden=True)
+    with np.errstate(invalid="ignore"):
+        wy, wh = ro.project(*(o[k] for k in KEYS))
+        ay, ah = ro.project(*(_absolute(o)[k] for k in KEYS))
+        _check(y, wy, np.nan_to_num(ay), K + r, dtype, "y")
+        _check(h, wh, np.nan_to_num(ah), K, "f32", "hidden")
+    return wy
+
+
+def _backward(fsb, d, dtype, need_adapters=True):
+    c, o = _cuda(d), _f64(d)
+    (N, K), M, r = d["x"].shape, d["g"].shape[1], d["a"].shape[1]
+    gx, ga, gb = fsb.project_grad(c["g"], c["x"], c["w"], _adapters(fsb, c), c["ids"], need_adapters=need_adapters)
+    with np.errstate(invalid="ignore"):
+        wx, wa, wb = ro.project_grad(*(o[k] for k in GRAD_KEYS))
+        ax, aa, ab = (np.nan_to_num(v) for v in ro.project_grad(*(_absolute(o)[k] for k in GRAD_KEYS)))
+        _check(gx, wx, ax, M + 2 * r, dtype, "gx")
+        if need_adapters:
+            _check(ga, wa, aa, N + M, dtype, "ga")
+            _check(gb, wb, ab, N + K, dtype, "gb")
+    return wx, wa, wb
+
+
+def _infinite_factor(fsb, dtype, N, K, M, r, n):
+    print("infinite factor", dtype, N, K, M, r, n, flush=True)
+    d = _problem(N + K + r, dtype, N, K, M, r, n, "mixed")
+    d["b"][1, 5, r - 1], d["b"][1, 7, 0] = float("inf"), -float("inf")
+    assert np.isinf(_forward(fsb, d, dtype)).any()
+    d = _problem(N + K + r, dtype, N, M, K, r, n, "mixed")
+    d["a"][1, r - 1, 5], d["a"][1, 0, 7] = float("inf"), -float("inf")
+    assert np.isinf(_backward(fsb, d, dtype)[0]).any()
+
+
+@pytest.mark.parametrize("N,K,M,r,n", FEW + TILES + SPLIT)
+def test_infinite_factor_f32(fsb, N, K, M, r, n):
+    """An infinite element of a factor gives the infinities of the definition, at ranks that leave operands unfilled."""
+    _infinite_factor(fsb, "f32", N, K, M, r, n)
