@@ -55,6 +55,28 @@ __device__ __forceinline__ void split_operand(const float *v, Operand<uint16_t> 
     }
 }
 
+// The adapter's part of four columns of a row, added to y term by term.  Seldom
+// taken: its addresses are kept from being computed ahead and held in registers.
+template <typename T, bool TRANS>
+__device__ __forceinline__ void add_adapter(const WideArgs &a, int64_t row, int col, float (&y)[4])
+{
+    asm volatile("" : "+v"(row), "+v"(col));
+    const int id = a.ids[row];
+    if (id < 0 || id >= a.n) return;
+    const T *f = reinterpret_cast<const T *>(a.f) + (int64_t)id * a.cols * a.r;
+    const float *t = a.t + row * a.r, sc = !TRANS && a.scale ? a.scale[id] : 1.f;
+    float z[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 1
+    for (int j = 0; j < a.r; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int c = min(col + e, a.cols - 1);
+            z[e] = fmaf(t[j], to_f32(TRANS ? f[(int64_t)j * a.cols + c] : f[(int64_t)c * a.r + j]), z[e]);
+        }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) y[e] = fmaf(z[e], sc, y[e]);
+}
+
 // WR x WC waves; two of them to a SIMD, 256 registers each.
 template <typename T, bool TRANS, int BM, int BN, int WR, int WC>
 __global__ __launch_bounds__(64 * WR * WC, 2) void project_tiles(WideArgs a, int tiles_m, int tiles_n, int per_split)
@@ -192,6 +214,7 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void project_tiles(WideArgs a, int
     bool bad = false;  // one of the lane's rows names an adapter that is not there
 #pragma unroll
     for (int i = 0; i < WM; ++i) bad |= a.n && id[i] >= a.n;
+    int again = 0;  // the lane's rows (bit i) whose adapter's part is added at the end
     if (a.n && per_split >= a.C) {
         for (int last = -1;;) {
             int low = 0x7fffffff;
@@ -215,8 +238,6 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void project_tiles(WideArgs a, int
                     const int col = min(n0 + wn + j * 16 + q, a.cols - 1);
                     of[j] = TRANS ? gather_operand(f + (int64_t)at * a.cols + col, a.cols, have)
                                   : load_operand(f + (int64_t)col * a.r + at, have);
-                    // past the rank both operands are 0: 0 times an infinity is none
-                    if (even) of[j].v = k < a.r ? of[j].v : decltype(of[j].v){};
                 }
 #pragma unroll
                 for (int h = 0; h < WM; h += H) {
@@ -252,6 +273,26 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void project_tiles(WideArgs a, int
                 }
             }
         }
+    }
+
+    // A row where that is not finite gets it at the end instead, term by term:
+    // these products also have terms that the definition does not, 0 in exact
+    // arithmetic but NaN beside an infinity.  They are the lanes past the rank (the
+    // factor's last values once more, times 0) and, of a bf16 product, the second
+    // and third parts of a value (which an infinity does not have, nor a float32
+    // value that rounds to one).  Finite rows pay a look at the accumulators for
+    // it (without adapters too: inside the condition above the 256 x 256 tile
+    // spills 480 bytes a thread); masks on every operand instead: 550,000 x 242 -> 15, 13 mixed adapters,
+    // the gradients: 1173 us, without them 1063.
+#pragma unroll
+    for (int i = 0; i < WM; ++i) {
+        f4 zero = f4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int j = 0; j < WN; ++j) zero = __builtin_elementwise_fma(acc[i][j], f4{0.f, 0.f, 0.f, 0.f}, zero);
+        const bool off = zero[0] + zero[1] + zero[2] + zero[3] != 0.f;
+        again |= off ? 1 << i : 0;
+#pragma unroll
+        for (int j = 0; j < WN; ++j) acc[i][j] = off ? f4{0.f, 0.f, 0.f, 0.f} : acc[i][j];
     }
 
     auto read = [&](int at, int half, Operand<T>(&oa)[WM], Operand<T>(&ob)[WN]) {
@@ -374,6 +415,7 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void project_tiles(WideArgs a, int
             float out[4];
 #pragma unroll
             for (int e = 0; e < 4; ++e) out[e] = wrong ? NAN : acc[i][j][e] + bias[e];
+            if (again & 1 << i) add_adapter<T, TRANS>(a, row, col, out);
             T *to = reinterpret_cast<T *>(a.out) + row * a.os + col;
             if (col + 4 <= a.cols) store_words<4 * sizeof(T)>(to, pack<T, 4>(out));
             else {

@@ -58,3 +58,40 @@ def _infinite_factor(fsb, dtype, N, K, M, r, n):
 def test_infinite_factor_f32(fsb, N, K, M, r, n):
     """An infinite element of a factor gives the infinities of the definition, at ranks that leave operands unfilled."""
     _infinite_factor(fsb, "f32", N, K, M, r, n)
+
+
+@pytest.mark.parametrize("N,K,M,r,n", FEW + TILES + SPLIT)
+def test_infinite_factor_bf16(fsb, N, K, M, r, n):
+    """The same where the hidden values are taken as three bf16 parts of either sign."""
+    _infinite_factor(fsb, "bf16", N, K, M, r, n)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("N,K,M,r,n", FEW + TILES + SPLIT)
+def test_infinite_hidden_values(fsb, dtype, N, K, M, r, n):
+    """A_i x, and in the gradient B_i^T g, of +-infinity."""
+    print("infinite hidden", dtype, N, K, M, r, n, flush=True)
+    d = _problem(N + K + r, dtype, N, K, M, r, n, "mixed")
+    d["a"][1, r - 1, 3] = float("inf")
+    assert np.isinf(_forward(fsb, d, dtype)).any()
+    d = _problem(N + K + r, dtype, N, M, K, r, n, "mixed")
+    d["b"][1, 5, r - 1] = float("inf")
+    assert np.isinf(_backward(fsb, d, dtype)[0]).any()
+
+
+@pytest.mark.parametrize("N,K,M,r,n", FEW + TILES + SPLIT)
+def test_hidden_values_past_the_largest_bf16(fsb, N, K, M, r, n):
+    """Finite float32 values that would round to an infinite bf16: 3.4015e38, times 2^-20."""
+    print("large hidden", N, K, M, r, n, flush=True)
+    d = _problem(N + K + r, "bf16", N, K, M, r, n, "mixed", scale=False)
+    d["x"][:, :2] = 1
+    d["a"][1, 0] = 0
+    d["a"][1, 0, 0], d["a"][1, 0, 1] = torch.finfo(torch.bfloat16).max, 1.2e36
+    d["b"][1, :, 0] *= 2.0 ** -20
+    assert np.abs(_forward(fsb, d, "bf16")).max() > 1e31
+    d = _problem(N + K + r, "bf16", N, M, K, r, n, "mixed", scale=False)
+    d["g"][:, :2] = 1
+    d["b"][1, :, 0] = 0
+    d["b"][1, 0, 0], d["b"][1, 1, 0] = torch.finfo(torch.bfloat16).max, 1.2e36
+    d["a"][1, 0] *= 2.0 ** -20
+    assert np.abs(_backward(fsb, d, "bf16", need_adapters=False)[0]).max() > 1e31
