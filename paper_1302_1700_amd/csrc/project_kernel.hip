@@ -423,7 +423,8 @@ __global__ __launch_bounds__(256) void factor_grad(FactorArgs<T> a)
                         float u = 0.f;
 #pragma unroll
                         for (int m = 0; m < MB; ++m) u = fmaf(__shfl(gv[k], (lane & 48) + m), bi[m], u);
-                        tv[k][0] = u;
+                        // no row, no term: 0 times an infinite factor would be NaN
+                        tv[k][0] = l + k * 4 + g < total ? u : 0.f;
                     }
 #pragma unroll
                     for (int p = 0; p < 4; ++p)

@@ -95,3 +95,16 @@ def test_hidden_values_past_the_largest_bf16(fsb, N, K, M, r, n):
     d["b"][1, 0, 0], d["b"][1, 1, 0] = torch.finfo(torch.bfloat16).max, 1.2e36
     d["a"][1, 0] *= 2.0 ** -20
     assert np.abs(_backward(fsb, d, "bf16", need_adapters=False)[0]).max() > 1e31
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("N,K,M,r", [(70, 48, 2, 4), (70, 48, 10, 9), (70, 48, 100, 9), (1030, 48, 2, 4), (1030, 33, 12, 16),
+                                     (1030, 48, 30, 20)])
+def test_factor_gradients_of_one_row_with_an_infinite_factor(fsb, dtype, N, K, M, r):
+    """An adapter of one row: its gradient is that row's outer product, infinite where B_i^T g is."""
+    print("one row an adapter", dtype, N, K, M, r, flush=True)
+    d = _problem(N + K + r, dtype, N, K, M, r, N, "runs")
+    assert (d["ids"] == torch.arange(N)).all()
+    d["b"][3, 0, r - 2], d["b"][N - 1, 1, 0] = float("inf"), -float("inf")
+    _, wa, _ = _backward(fsb, d, dtype)
+    assert np.isinf(wa[3, r - 2]).all() and np.isinf(wa[N - 1, 0]).all()
