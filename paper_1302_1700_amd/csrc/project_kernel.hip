@@ -334,10 +334,11 @@ __device__ __forceinline__ void four(const T *v, int c, int C, bool have, float 
 }
 
 // Where sums go: the part of a run, or the gradient itself when there is one
-// run; four adjacent columns of rank j.
+// run (times the adapter's scale, unless it is the sum of no rows, 0 at any
+// scale); four adjacent columns of rank j.
 template <typename T>
 __device__ __forceinline__ void store_sums(const FactorArgs<T> &a, const FactorJob<T> &job, int64_t unit, int i, int j, int c,
-                                           f4 s)
+                                           f4 s, bool seen)
 {
     if (j >= a.r) return;
     if (a.runs > 1 && c + 4 <= job.C) {
@@ -350,7 +351,7 @@ __device__ __forceinline__ void store_sums(const FactorArgs<T> &a, const FactorJ
         if (a.runs > 1) job.parts[(unit * a.r + j) * job.C + c + e] = s[e];
         else
             store_as(job.out + (job.by_rank ? ((int64_t)i * a.r + j) * job.C + c + e : ((int64_t)i * job.C + c + e) * a.r + j),
-                     job.scale ? s[e] * job.scale[i] : s[e]);
+                     job.scale && seen ? s[e] * job.scale[i] : s[e]);
     }
 }
 
@@ -467,14 +468,14 @@ __global__ __launch_bounds__(256) void factor_grad(FactorArgs<T> a)
 #pragma unroll
             for (int e = 0; e < 4; ++e)
                 store_sums(a, job, unit, i, j * 16 + g * 4 + e, c0 + q * 4,
-                           f4{acc[0][j][e], acc[1][j][e], acc[2][j][e], acc[3][j][e]});
+                           f4{acc[0][j][e], acc[1][j][e], acc[2][j][e], acc[3][j][e]}, seen);
         if (second && q < M) {
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 const int j = g * 4 + e;
                 if (j >= r) continue;
                 if (a.runs > 1) jb.parts[(unit * r + j) * M + q] = gb[e];
-                else store_as(jb.out + ((int64_t)i * M + q) * r + j, jb.scale ? gb[e] * jb.scale[i] : gb[e]);
+                else store_as(jb.out + ((int64_t)i * M + q) * r + j, jb.scale && seen ? gb[e] * jb.scale[i] : gb[e]);
             }
         }
     }
@@ -495,8 +496,10 @@ __global__ __launch_bounds__(256) void factor_join(FactorArgs<T> a)
         const int i = (int)(unit / blocks), k = (int)(unit - (int64_t)i * blocks) * 64 + lane;
         const float *parts = job.parts + (int64_t)i * a.runs * per_adapter + std::min(k, per_adapter - 1);
         float s = 0.f;
+        bool seen = false;
         for (int at = 0; at < a.runs; at += 1024) {
             const int total = list_rows<4>(a.used + (int64_t)i * a.runs, at, a.runs, 1, list, count, [](int64_t, int) {});
+            seen |= total > 0;
             const int quarter = (total + 3) / 4, to = std::min(total, (wave + 1) * quarter);
             for (int l = wave * quarter; l < to; l += 8) {
                 float v[8];  // in flight together
@@ -511,7 +514,7 @@ __global__ __launch_bounds__(256) void factor_join(FactorArgs<T> a)
         __syncthreads();
         if (wave == 0 && k < per_adapter) {
             s = (sums[0][lane] + sums[1][lane]) + (sums[2][lane] + sums[3][lane]);
-            if (job.scale) s *= job.scale[i];
+            if (job.scale && seen) s *= job.scale[i];  // 0 at any scale where no row names the adapter
             const int j = k / job.C, c = k - j * job.C;
             store_as(job.out + (int64_t)i * per_adapter + (job.by_rank ? k : c * a.r + j), s);
         }

@@ -108,3 +108,16 @@ def test_factor_gradients_of_one_row_with_an_infinite_factor(fsb, dtype, N, K, M
     d["b"][3, 0, r - 2], d["b"][N - 1, 1, 0] = float("inf"), -float("inf")
     _, wa, _ = _backward(fsb, d, dtype)
     assert np.isinf(wa[3, r - 2]).all() and np.isinf(wa[N - 1, 0]).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("N", [0, 70, 1030])
+@pytest.mark.parametrize("K,M,r", [(48, 2, 4), (48, 30, 20)])
+def test_adapters_without_rows_have_zero_gradients_at_any_scale(fsb, dtype, N, K, M, r):
+    d = _problem(N + K + r, dtype, N, K, M, r, 4, "runs")
+    d["ids"][d["ids"] == 1] = 0
+    d["ids"][d["ids"] == 2] = -1
+    d["scale"] = torch.tensor([1.0, float("inf"), float("nan"), 0.5])
+    print("no rows, scales not finite", dtype, N, K, M, r, flush=True)
+    _, wa, wb = _backward(fsb, d, dtype)
+    assert (wa[1:3] == 0).all() and (wb[1:3] == 0).all()
