@@ -363,7 +363,8 @@ __device__ __forceinline__ void store_sums(const FactorArgs<T> &a, const FactorJ
 // waves share the rows and their sums are joined in LDS.  Two jobs (both
 // factors) by blockIdx.x; FUSED (M and r up to 16; MB: M's bound) makes both in
 // one pass over the rows: lane q holds column q of its adapter's B and makes
-// u = B^T g of its row from the row's 16 lanes, so u never goes through memory.
+// B^T g of its row from the row's 16 lanes, so it never goes through memory;
+// both sums take the scale at the end.
 template <int NB>
 constexpr int kGroups = NB == 1 ? 8 : NB == 2 ? 4 : 2;
 
@@ -385,9 +386,8 @@ __global__ __launch_bounds__(256) void factor_grad(FactorArgs<T> a)
         const int64_t begin = run * a.run_rows, end = std::min(a.rows, begin + a.run_rows);
         float bi[FUSED ? MB : 1];
         if constexpr (FUSED) {
-            const float sc = jb.scale ? jb.scale[i] : 1.f;
 #pragma unroll
-            for (int m = 0; m < MB; ++m) bi[m] = m < M && q < r ? to_f32(a.b[((int64_t)i * M + m) * r + q]) * sc : 0.f;
+            for (int m = 0; m < MB; ++m) bi[m] = m < M && q < r ? to_f32(a.b[((int64_t)i * M + m) * r + q]) : 0.f;
         }
         f4 acc[4][NB], gb = f4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
@@ -687,7 +687,8 @@ hipError_t project_grad(const ProjArgs &a, int dtype, const T *g, int64_t gs, co
     if (ga) {
         const RunPlan p = run_plan(a);
         FactorArgs<T> f{};
-        f.job[0] = FactorJob<T>{u, (const T *)a.x, a.xs, a.K, 1, 0, nullptr, ga, (float *)ws};
+        // u has the scale already where it goes through memory
+        f.job[0] = FactorJob<T>{u, (const T *)a.x, a.xs, a.K, 1, 0, fused ? a.scale : nullptr, ga, (float *)ws};
         f.job[1] = FactorJob<T>{h, g, gs, a.M, 0, 0, a.scale, gb, (float *)(ws + p.parts[0])};
         f.rows = a.rows;
         f.run_rows = p.run_rows;

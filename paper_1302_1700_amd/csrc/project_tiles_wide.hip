@@ -259,7 +259,7 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void project_tiles(WideArgs a, int
                         if (!__any(hit)) continue;
                         Operand<T> ot[Q];
 #pragma unroll
-                        for (int e = 0; e < E; ++e) tv[i][e] = k < a.r ? tv[i][e] * sc : 0.f;
+                        for (int e = 0; e < E; ++e) tv[i][e] = k < a.r ? tv[i][e] : 0.f;
                         split_operand(tv[i], ot);
 #pragma unroll
                         for (int j = 0; j < WN; ++j) {
@@ -267,7 +267,10 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void project_tiles(WideArgs a, int
 #pragma unroll
                             for (int p = 0; p < Q; ++p) z = block_product(of[j], ot[p], z);
 #pragma unroll
-                            for (int e = 0; e < 4; ++e) acc[h + i][j][e] += hit ? z[e] : 0.f;
+                            for (int e = 0; e < 4; ++e) {
+                                const float y = acc[h + i][j][e];
+                                acc[h + i][j][e] = TRANS ? y + (hit ? z[e] : 0.f) : hit ? fmaf(z[e], sc, y) : y;
+                            }
                         }
                     }
                 }
@@ -291,8 +294,12 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void project_tiles(WideArgs a, int
         for (int j = 0; j < WN; ++j) zero = __builtin_elementwise_fma(acc[i][j], f4{0.f, 0.f, 0.f, 0.f}, zero);
         const bool off = zero[0] + zero[1] + zero[2] + zero[3] != 0.f;
         again |= off ? 1 << i : 0;
+    }
+    if (BUFFER || __any(again)) {  // (as a branch the largest tile spills)
 #pragma unroll
-        for (int j = 0; j < WN; ++j) acc[i][j] = off ? f4{0.f, 0.f, 0.f, 0.f} : acc[i][j];
+        for (int i = 0; i < WM; ++i)
+#pragma unroll
+            for (int j = 0; j < WN; ++j) acc[i][j] = again & 1 << i ? f4{0.f, 0.f, 0.f, 0.f} : acc[i][j];
     }
 
     auto read = [&](int at, int half, Operand<T>(&oa)[WM], Operand<T>(&ob)[WN]) {

@@ -121,3 +121,20 @@ def test_adapters_without_rows_have_zero_gradients_at_any_scale(fsb, dtype, N, K
     print("no rows, scales not finite", dtype, N, K, M, r, flush=True)
     _, wa, wb = _backward(fsb, d, dtype)
     assert (wa[1:3] == 0).all() and (wb[1:3] == 0).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("N,K,M,r,n", FEW + TILES + SPLIT + [(70, 48, 2, 4, 3), (600, 48, 12, 9, 3)])
+def test_scale_multiplies_the_sum(fsb, dtype, N, K, M, r, n):
+    """s (B h) of 2^80 where s times a hidden value, or a factor's element, would pass float32's range."""
+    print("large scale", dtype, N, K, M, r, n, flush=True)
+    d = _problem(N + K + r, dtype, N, K, M, r, n, "mixed")
+    d["scale"] *= 2.0 ** 40
+    d["a"] *= 2.0 ** 100
+    d["b"] *= 2.0 ** -60
+    assert np.abs(_forward(fsb, d, dtype)).max() < 2.0 ** 100
+    d = _problem(N + K + r, dtype, N, K, M, r, n, "mixed")
+    d["scale"] *= 2.0 ** 40
+    d["b"] *= 2.0 ** 100
+    d["g"] *= 2.0 ** -60
+    assert np.abs(_backward(fsb, d, dtype)[1]).max() < 2.0 ** 110
