@@ -138,3 +138,39 @@ def test_scale_multiplies_the_sum(fsb, dtype, N, K, M, r, n):
     d["b"] *= 2.0 ** 100
     d["g"] *= 2.0 ** -60
     assert np.abs(_backward(fsb, d, dtype)[1]).max() < 2.0 ** 110
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("N,K,M,r,n", FEW + TILES + SPLIT)
+def test_infinities_stay_with_their_rows(fsb, dtype, N, K, M, r, n):
+    """NaN and infinities in a row, a gradient row, or an adapter change nothing of the other rows and adapters."""
+    print("isolation", dtype, N, K, M, r, n, flush=True)
+    bits = lambda t: t.view(torch.int16 if t.dtype == torch.bfloat16 else torch.int32)
+
+    def spoil(c):
+        c["x"][5, 3], c["x"][6, 4] = float("nan"), float("inf")
+        c["g"][7, 1], c["g"][8, 2] = float("nan"), -float("inf")
+        c["a"][1, r - 1, 7], c["b"][1, 3, 0] = float("nan"), float("inf")
+
+    c = _cuda(_problem(N + r, dtype, N, K, M, r, n, "mixed"))
+    clean = fsb.project(c["x"], c["w"], None, _adapters(fsb, c), c["ids"], return_hidden=True)
+    spoil(c)
+    got = fsb.project(c["x"], c["w"], None, _adapters(fsb, c), c["ids"], return_hidden=True)
+    rest = c["ids"] != 1
+    rest[5] = rest[6] = False
+    for g, w in zip(got, clean):
+        assert torch.equal(bits(g[rest]), bits(w[rest]))
+    c = _cuda(_problem(N + r, dtype, N, M, K, r, n, "mixed"))
+    clean = fsb.project_grad(c["g"], c["x"], c["w"], _adapters(fsb, c), c["ids"])
+    spoil(c)
+    got = fsb.project_grad(c["g"], c["x"], c["w"], _adapters(fsb, c), c["ids"])
+    rest = c["ids"] != 1
+    rest[7] = rest[8] = False
+    assert torch.equal(bits(got[0][rest]), bits(clean[0][rest]))
+    rest = torch.ones(n, dtype=torch.bool, device="cuda")
+    rest[1] = False
+    for row in (5, 6, 7, 8):
+        if c["ids"][row] >= 0:
+            rest[c["ids"][row].long()] = False
+    for g, w in zip(got[1:], clean[1:]):
+        assert torch.equal(bits(g[rest]), bits(w[rest]))
