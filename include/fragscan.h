@@ -395,8 +395,9 @@ fs_status fs_reassembly_index(const fs_net *net, int32_t H, int32_t W, int32_t *
  *                    and their log probabilities
  * A score of -inf rules its class out (probability 0, never listed: places no
  * class takes hold -1 and -inf).  A row of nothing but -inf has norm (-inf,
- * 0), entropy 0, log probability -inf for every label and an empty list.  A
- * row that holds a NaN or +inf gives NaN throughout and -1 in its list.
+ * 0), entropy 0, log probability -inf for every label below classes and an
+ * empty list.  A row that holds a NaN or +inf gives NaN throughout (0 still
+ * for a negative label) and -1 in its list.
  * Any output may be NULL if another is not; d_logp needs d_labels.
  * FS_ERR_INVALID_ARG for a temperature outside 1e-30 .. 1e30, n_top outside 0 .. FS_MAX_TOP, classes outside 1 ..
  * FS_MAX_CLASSES. */
@@ -411,10 +412,10 @@ fs_status fs_logprobs(const void *d_scores, int64_t rows, int32_t classes, int64
  * from the same scores, labels and temperature, fs_logprobs' d_norm, and the
  * gradients of its outputs d_g_logp [rows] (needs d_labels) and d_g_entropy
  * [rows] (needs d_entropy, fs_logprobs' own); either may be NULL, not both.
- * Rows without a label take no part of d_g_logp; rows of nothing but -inf
- * have gradient 0; rows of NaN or +inf, and rows whose label is >= classes
- * when d_g_logp is given, NaN.  d_g_scores may be d_scores itself with the
- * same stride. */
+ * Rows without a label take no part of d_g_logp; rows of NaN or +inf, and rows
+ * whose label is >= classes when d_g_logp is given, have gradient NaN; other
+ * rows of nothing but -inf have gradient 0.  d_g_scores may be d_scores itself
+ * with the same stride. */
 fs_status fs_logprobs_grad(const void *d_scores, int64_t rows, int32_t classes, int64_t stride, int32_t dtype,
                            float temperature, const int32_t *d_labels, const float *d_norm, const float *d_entropy,
                            const float *d_g_logp, const float *d_g_entropy, void *d_g_scores, int64_t g_stride,
@@ -428,7 +429,8 @@ fs_status fs_logprobs_grad(const void *d_scores, int64_t rows, int32_t classes, 
  * weights); d_bias float [m] or NULL; d_a [n_adapters][rank][k] and d_b
  * [n_adapters][m][rank], contiguous; d_scale float [n_adapters] or NULL for
  * ones; d_ids int32 [rows].  n_adapters = 0: no adapters, rank 0, the factor
- * and id pointers NULL. */
+ * and id pointers NULL.  NaN and infinities in a row or an adapter change
+ * nothing of the rows, and of the adapters' gradients, that do not use it. */
 typedef struct {
     int64_t rows;
     int32_t k;

@@ -5,7 +5,8 @@
 // D = sum exp(d_j) d_j: log p_j = d_j - ln S and the entropy is ln S - D / S,
 // two terms >= 0, so nothing cancels where the scores are far from 0.  The
 // kernels keep d in units of log2 (one factor k = log2(e) / T, the hardware's
-// exp2) and D with it.  Every row is read once.
+// exp2) and D with it.  Every row is read once; of a long row whose best classes
+// are listed, the scores of the threads that may hold them a second time.
 //
 // A score of -inf has exp 0; its d is held at -1e30 where it multiplies that 0.
 // Maxima start from the lowest finite float, so -inf never meets -inf; S = 0
@@ -593,8 +594,9 @@ __global__ __launch_bounds__(256) void logprobs_grad_long(LogprobGradArgs a, int
 int capped(int64_t blocks) { return (int)std::max<int64_t>(1, std::min<int64_t>(blocks, 1 << 22)); }
 
 // -- choices -------------------------------------------------------------------
-// Classes a wave's registers hold at 8 a lane.  20,000 x 500 float32: 11 us, as
-// long rows of four waves 51; the 5 best 32 and 133.
+// Classes a wave's registers hold at 8 a lane.  20,000 x 500 float32: 12 us, as
+// long rows of one wave 18; the best one 16 and 35, the 5 best 30 and 37, the 64
+// best, a group maximum each, 242 and 198 (20,000 x 400 bf16: 239 and 412).
 constexpr int kShort = 512;
 
 struct LongPlan {

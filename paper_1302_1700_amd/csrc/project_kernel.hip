@@ -1,8 +1,9 @@
 // A fully connected layer on rows with a low-rank adapter of each row's own
 // choice, and its gradient:  y = W x + bias + s_i B_i (A_i x), i = ids[row].
 //
-// Few outputs (m + rank up to 64): one pass over the rows, in which the rows
-// of W and of A_i are the columns of one product (project_narrow); more: the
+// Few outputs (m + rank up to 64): one kernel, in which the rows of W and of A_i
+// are the columns of one product (project_narrow; rows of more adapters than the
+// columns have room for are multiplied again, from the caches); more: the
 // rows times A_i first (rank_rows), then a tiled product that adds B_i's part
 // (project_tiles_wide.hip).  The factors' gradients: per adapter, sums over its rows
 // of outer products, in runs of rows joined by a second launch in the order of
@@ -54,7 +55,7 @@ __device__ __forceinline__ void row_products(const T *const (&row)[RB], const T 
 
 // The rows of one adapter among 1024: their offsets from the first, in order, in
 // `list`; returns how many.  All threads of the workgroup take part (NW waves);
-// `id` is called with every row's adapter once: id(row, adapter).
+// `each` is called with every row's adapter once: each(row, adapter).
 template <int NW, typename Id, typename Each>
 __device__ __forceinline__ int list_rows(const Id *ids, int64_t at, int64_t end, int adapter, int *list, int *count,
                                          Each each)
@@ -169,7 +170,8 @@ __global__ __launch_bounds__(W > 4 ? 64 * W : 256) void rank_rows(RankArgs<T> a)
 }
 
 // Few outputs: columns 0 .. M - 1 of the product are W's rows, the next ones
-// the rows of as many of the tile's adapters' A as fit; the products go through
+// the rows of as many of the tile's adapters' A as fit (the others in further
+// passes over the tile's rows); the products go through
 // LDS, where each row's outputs take up their hidden values.  A wave takes 16 RB
 // rows (W = 1), or 16 shared by W waves.
 template <typename T, int RB, int NB, int W>
@@ -525,8 +527,14 @@ __global__ __launch_bounds__(256) void factor_join(FactorArgs<T> a)
 size_t up256(size_t v) { return (v + 255) & ~(size_t)255; }
 size_t rank_bytes(const ProjArgs &a) { return up256((size_t)a.rows * a.r * sizeof(float)); }
 
-// W's and A's rows as columns of one product: 1M x 200 -> 20 float32, rank 8: 488
-// us, rows times A first and tiles of 64 columns then 805.
+// W's and A's rows as columns of one product.  Adapters in runs: 1M x 200 -> 20
+// float32, rank 8: 498 us (its bytes at a copy's rate: 186), rows times A first
+// and tiles of 64 columns then 817; 300,000 x 200 -> 2, rank 16, 64 adapters: 97
+// and 359; a long axis of few rows, 4093 x 4096 -> 40 bf16, rank 16: 59 and 47.
+// In any order the columns are multiplied again for every few adapters that 16 or
+// 32 rows name, and this way loses where these are many: the same 300,000 rows
+// 1882 and 625, with 8 adapters 576 and 358, at rank 4 141 and 351; 4093 x 4096 ->
+// 40 175 and 60.  The order of the ids is not known here.
 bool narrow(const ProjArgs &a) { return a.M + a.r <= 64; }
 
 // Waves that share the summed axis of a product: the fewer rows and the longer
@@ -542,7 +550,7 @@ int axis_waves(int64_t rows, int C)
     return steps >= 8 && rows <= (steps >= 64 ? 65536 : 16384) ? 4 : 1;
 }
 
-// Both factors' gradients in one pass: 1M x 200 -> 2 float32, rank 4: 247 us, with
+// Both factors' gradients in one pass: 1M x 200 -> 2 float32, rank 4: 237 us, with
 // the ranks' rows through memory and two passes 548.
 bool both(const ProjArgs &a) { return a.M <= 16 && a.r <= 16; }
 

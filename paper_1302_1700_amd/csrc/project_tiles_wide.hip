@@ -1,12 +1,14 @@
 // The shared projection's matrix product with the adapters' part added to its
 // accumulators: out = v W + t F_i, i the adapter of the row.
 //
-// A workgroup computes a BM x BN tile, its four waves a quarter each.  The
-// summed axis is walked 128 bytes of each row at a time through two LDS
-// buffers: while a step's products run, the next one is written to LDS from
-// registers and the one after that is on its way from memory.  A step is two
-// halves; each half's operands are read while the other half's products run,
-// so one barrier a step suffices and no product waits for LDS.
+// A workgroup of WR x WC waves computes a BM x BN tile, a part of BM / WR x BN /
+// WC each wave: four waves for tiles of 64 and 128, eight for 256.  The summed
+// axis is walked 128 bytes of each row at a time through two LDS buffers: while
+// a step's products run, the next one is written to LDS from registers and the
+// one after that is on its way from memory; one barrier a step.  A step is two
+// halves.  In the smaller tiles each half's operands are read while the other
+// half's products run, and no product waits for LDS.  The 256 x 256 tile has no
+// registers for a second set of operands: it reads a half, waits, multiplies.
 //
 // LDS keeps a row's 16-byte pieces in an order turned by the row (piece p of
 // row q at p ^ (q % 8)), so that the 16 rows an operand load touches fall on
@@ -285,8 +287,8 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void project_tiles(WideArgs a, int
     // and third parts of a value (which an infinity does not have, nor a float32
     // value that rounds to one).  Finite rows pay a look at the accumulators for
     // it (without adapters too: inside the condition above the 256 x 256 tile
-    // spills 480 bytes a thread); masks on every operand instead: 550,000 x 242 -> 15, 13 mixed adapters,
-    // the gradients: 1173 us, without them 1063.
+    // spills 480 bytes a thread); masks on every operand instead: 550,000 x 242 ->
+    // 15, 13 mixed adapters, the gradients: 1173 us, without them 1063.
 #pragma unroll
     for (int i = 0; i < WM; ++i) {
         f4 zero = f4{0.f, 0.f, 0.f, 0.f};
