@@ -174,3 +174,19 @@ def test_infinities_stay_with_their_rows(fsb, dtype, N, K, M, r, n):
             rest[c["ids"][row].long()] = False
     for g, w in zip(got[1:], clean[1:]):
         assert torch.equal(bits(g[rest]), bits(w[rest]))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("N,K,M,r,n", FEW + TILES + SPLIT + [(70, 48, 2, 4, 3), (1030, 48, 12, 9, 3)])
+def test_infinite_rows(fsb, dtype, N, K, M, r, n):
+    """An infinite element of a row, or of its gradient, with an adapter and without one."""
+    print("infinite rows", dtype, N, K, M, r, n, flush=True)
+    d = _problem(N + r, dtype, N, K, M, r, n, "mixed")
+    d["ids"][5], d["ids"][6] = -1, 1
+    d["x"][5, 3], d["x"][6, 4] = float("inf"), -float("inf")
+    assert np.isinf(_forward(fsb, d, dtype)[5]).all()
+    d = _problem(N + r, dtype, N, M, K, r, n, "mixed")
+    d["ids"][5], d["ids"][6], d["ids"][7] = -1, 1, 0
+    d["g"][5, 1], d["g"][6, 0], d["x"][7, 1] = float("inf"), -float("inf"), float("inf")
+    wx, _, wb = _backward(fsb, d, dtype)
+    assert np.isinf(wx[5]).all() and np.isinf(wb[1, 0]).all()
